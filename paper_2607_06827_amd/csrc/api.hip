@@ -11,6 +11,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "host_checks.hpp"
 #include "kernels.hpp"
 #include "kernels_bwd.hpp"
 #include "kernels_fused.hpp"
@@ -24,33 +25,7 @@ static __device__ __align__(256) unsigned char scratch[SPEECHKV_NOALLOC_SCRATCH_
 
 namespace {
 
-constexpr int kMaxGrid = 65535;
-constexpr int kMaxRows = 2147483647 - SPEECHKV_MAX_WINDOW;  // ceil(T / w) stays in int32
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int elt_size(int dtype) { return dtype == SPEECHKV_DTYPE_BF16 ? 2 : 4; }
-
-int log2_exact(int x) {
-  int s = 0;
-  while ((1 << s) < x) ++s;
-  return (1 << s) == x ? s : -1;
-}
-
-// Checks shared by every call on the cache description.
-int check_cache(const speechkv_paged_kv* c) {
-  if (!c || !c->k_pages || !c->v_pages || !c->block_table) return SPEECHKV_ERR_INVALID_ARG;
-  if (c->num_pages < 1 || c->max_pages_per_seq < 1 || c->num_kv_heads < 1)
-    return SPEECHKV_ERR_INVALID_ARG;
-  if (c->dtype != SPEECHKV_DTYPE_F32 && c->dtype != SPEECHKV_DTYPE_BF16) return SPEECHKV_ERR_UNSUPPORTED;
-  if (c->head_dim != 64 && c->head_dim != 128) return SPEECHKV_ERR_UNSUPPORTED;
-  if (c->page_size < 8 || c->page_size > 256 || log2_exact(c->page_size) < 0)
-    return SPEECHKV_ERR_UNSUPPORTED;
-  if (c->num_kv_heads > kMaxGrid) return SPEECHKV_ERR_UNSUPPORTED;
-  if ((int64_t)c->max_pages_per_seq * c->page_size > INT32_MAX) return SPEECHKV_ERR_INVALID_ARG;
-  if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return SPEECHKV_ERR_INVALID_ARG;
-  return SPEECHKV_OK;
-}
+using namespace skv;
 
 int check_spans(const speechkv_spans* s) {
   if (!s || !s->prefix_len || !s->speech_len || !s->suffix_len) return SPEECHKV_ERR_INVALID_ARG;
@@ -90,21 +65,6 @@ speechkv_spans spans_of(const speechkv_segments* g) {
   return s;
 }
 
-skv::PagedView view_of(const speechkv_paged_kv* c) {
-  skv::PagedView v;
-  v.num_pages = c->num_pages;
-  v.page_shift = log2_exact(c->page_size);
-  v.max_pages = c->max_pages_per_seq;
-  v.kv_heads = c->num_kv_heads;
-  return v;
-}
-
-int group_of(int num_q_heads, int num_kv_heads) {
-  if (num_q_heads < 1 || num_q_heads % num_kv_heads) return -1;
-  const int g = num_q_heads / num_kv_heads;
-  return (g == 1 || g == 2 || g == 4 || g == 8) ? g : -1;
-}
-
 // Whether speechkv_pool_prefill_attn runs as one kernel that pools each key
 // tile it reads, or as two, the pooling and then the attention over the cache.
 // One kernel saves a launch (calls through the binding in a row are bound by
@@ -141,35 +101,6 @@ bool pool_prefill_one_kernel(int head_dim, int group, int64_t pairs, int w_eff, 
   if (head_dim == 64) return key_tiles <= (w_eff == 1 ? 6 : 2);
   const bool one_row_tile = group == 8 || rows <= skv::prefill_rows_per_tile(SPEECHKV_DTYPE_BF16, group);
   return one_row_tile && (w_eff == 1 || key_tiles <= 1);
-}
-
-int64_t page_pool_bytes(const speechkv_paged_kv* c) {
-  return (int64_t)c->num_pages * c->num_kv_heads * c->page_size * c->head_dim * elt_size(c->dtype);
-}
-
-bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + (uintptr_t)nb && b0 < a0 + (uintptr_t)na;
-}
-
-int status_of(hipError_t e) { return e == hipSuccess ? SPEECHKV_OK : SPEECHKV_ERR_HIP; }
-
-// A byte range of one argument; a null pointer takes no part in the checks.
-struct Region {
-  const void* p;
-  int64_t n;
-};
-
-// True when a written region overlaps a read region or another written one.
-bool aliased(const Region* wr, int nw, const Region* rd, int nr) {
-  for (int i = 0; i < nw; ++i) {
-    if (!wr[i].p) continue;
-    for (int k = 0; k < nr; ++k)
-      if (rd[k].p && overlaps(wr[i].p, wr[i].n, rd[k].p, rd[k].n)) return true;
-    for (int k = i + 1; k < nw; ++k)
-      if (wr[k].p && overlaps(wr[i].p, wr[i].n, wr[k].p, wr[k].n)) return true;
-  }
-  return false;
 }
 
 constexpr int kMaxDevices = 256;

@@ -1,0 +1,250 @@
+// C-ABI host layer of the steps of several new tokens
+// (include/speechkv_draft.h): argument validation, grid sizing and dispatch.
+// Every check runs before the first HIP call.
+#include "../../include/speechkv_draft.h"
+
+#include <algorithm>
+
+#include "host_checks.hpp"
+#include "kernels_draft.hpp"
+
+namespace {
+
+using namespace skv;
+
+// Bytes from the first to past the last element of a strided [batch][rows]
+// [heads][dim] tensor, or -1 when they do not fit 2^62 (no tensor is so long).
+int64_t extent(int64_t batch, int64_t sb, int64_t rows, int64_t ss, int64_t heads, int64_t sh, int64_t dim,
+               int64_t elt) {
+  const __int128 n = ((__int128)(batch - 1) * sb + (__int128)(rows - 1) * ss + (__int128)(heads - 1) * sh + dim) * elt;
+  return n < ((__int128)1 << 62) ? (int64_t)n : -1;
+}
+
+bool bad_stride(int64_t s, int64_t per16) { return s < 0 || s % per16; }
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int64_t table_bytes(const speechkv_paged_kv* c, int32_t batch) { return (int64_t)batch * c->max_pages_per_seq * 4; }
+
+}  // namespace
+
+extern "C" {
+
+int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s, int64_t q_stride_h,
+                       int32_t num_q_heads, const void* k, const void* v, int64_t stride_b, int64_t stride_s,
+                       int64_t stride_h, int32_t batch, int32_t num_new, const int32_t* new_len,
+                       const int32_t* positions, const float* inv_freq, int32_t rot_dim, int32_t rope,
+                       const int32_t* cache_len, const speechkv_paged_kv* cache, void* q_out,
+                       int32_t* cache_len_out, void* stream) {
+  if (!k || !v || !cache_len || (q == nullptr) != (q_out == nullptr)) return SPEECHKV_ERR_INVALID_ARG;
+  const int st = check_cache(cache);
+  if (st) return st;
+  if (batch < 1 || batch > kMaxGrid || num_new < 1) return SPEECHKV_ERR_INVALID_ARG;
+  if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return SPEECHKV_ERR_INVALID_ARG;
+  if (rope != SPEECHKV_ROPE_HALVES && rope != SPEECHKV_ROPE_PAIRS) return SPEECHKV_ERR_INVALID_ARG;
+  if (rot_dim && (!positions || !inv_freq)) return SPEECHKV_ERR_INVALID_ARG;
+  if (q) {
+    if (num_q_heads < 1 || num_q_heads % cache->num_kv_heads) return SPEECHKV_ERR_INVALID_ARG;
+    if (group_of(num_q_heads, cache->num_kv_heads) < 0) return SPEECHKV_ERR_UNSUPPORTED;
+  }
+  const int esz = elt_size(cache->dtype), D = cache->head_dim;
+  const int64_t per16 = 16 / esz;
+  if (bad_stride(stride_b, per16) || bad_stride(stride_s, per16) || bad_stride(stride_h, per16))
+    return SPEECHKV_ERR_INVALID_ARG;
+  if (q && (bad_stride(q_stride_b, per16) || bad_stride(q_stride_s, per16) || bad_stride(q_stride_h, per16)))
+    return SPEECHKV_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out)) return SPEECHKV_ERR_INVALID_ARG;
+  if (!aligned4(new_len) || !aligned4(positions) || !aligned4(inv_freq) || !aligned4(cache_len) ||
+      !aligned4(cache_len_out))
+    return SPEECHKV_ERR_INVALID_ARG;
+  const int64_t kv_bytes = extent(batch, stride_b, num_new, stride_s, cache->num_kv_heads, stride_h, D, esz);
+  const int64_t q_bytes = q ? extent(batch, q_stride_b, num_new, q_stride_s, num_q_heads, q_stride_h, D, esz) : 0;
+  const int64_t out_bytes =
+      q ? extent(batch, (int64_t)num_new * num_q_heads * D, num_new, (int64_t)num_q_heads * D, num_q_heads, D, D, esz)
+        : 0;
+  if (kv_bytes < 0 || q_bytes < 0 || out_bytes < 0) return SPEECHKV_ERR_INVALID_ARG;
+  // the queries may be rotated in place: a thread reads what it writes (a
+  // stride along an axis of length 1 does not matter)
+  const bool in_place = q && q == q_out && (num_q_heads == 1 || q_stride_h == D) &&
+                        (num_new == 1 || q_stride_s == (int64_t)num_q_heads * D) &&
+                        (batch == 1 || q_stride_b == (int64_t)num_new * num_q_heads * D);
+  const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;
+  const Region rd[] = {{in_place ? nullptr : q, q_bytes}, {k, kv_bytes}, {v, kv_bytes}, {new_len, lens},
+                       {rot_dim ? positions : nullptr, lens * num_new},
+                       {rot_dim ? inv_freq : nullptr, (int64_t)rot_dim * 2}, {cache_len, lens},
+                       {cache->block_table, table_bytes(cache, batch)}};
+  const Region wr[] = {{cache->k_pages, pool}, {cache->v_pages, pool}, {q_out, out_bytes}, {cache_len_out, lens}};
+  if (aliased(wr, 4, rd, 8)) return SPEECHKV_ERR_ALIAS;
+  AppendArgs a;
+  a.q = q;
+  a.q_stride_b = q_stride_b;
+  a.q_stride_s = q_stride_s;
+  a.q_stride_h = q_stride_h;
+  a.num_q_heads = q ? num_q_heads : 0;
+  a.k = k;
+  a.v = v;
+  a.stride_b = stride_b;
+  a.stride_s = stride_s;
+  a.stride_h = stride_h;
+  a.num_new = num_new;
+  a.new_len = new_len;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.rot = rot_dim;
+  a.pairs = rope == SPEECHKV_ROPE_PAIRS;
+  a.cache_len = cache_len;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.table = cache->block_table;
+  a.pv = view_of(cache);
+  a.q_out = q_out;
+  a.cache_len_out = cache_len_out;
+  return status_of(launch_append(a, cache->dtype, D, batch, static_cast<hipStream_t>(stream)));
+}
+
+int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
+                                 int32_t max_cache_len) {
+  if (batch < 1 || num_nodes < 1 || num_nodes > SPEECHKV_MAX_TREE_NODES || num_kv_heads < 1 ||
+      group_of(num_q_heads, num_kv_heads) < 0 || max_cache_len < 0)
+    return -1;
+  return 1;
+}
+
+size_t speechkv_tree_workspace_bytes(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
+                                     int32_t head_dim, int32_t max_cache_len, int32_t num_splits) {
+  if (head_dim < 1 || num_splits < 0) return 0;
+  const int32_t s = speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, max_cache_len);
+  if (s < 0) return 0;
+  const size_t splits = num_splits ? num_splits : s;
+  if (splits <= 1) return 0;
+  const size_t rows = (size_t)batch * num_nodes * num_q_heads * splits;
+  return rows * head_dim * sizeof(float) + rows * 2 * sizeof(float);
+}
+
+int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t num_q_heads,
+                       const speechkv_paged_kv* cache, const int32_t* cache_len, int32_t max_cache_len,
+                       const int32_t* num_nodes_of, const uint32_t* tree_mask, int64_t mask_stride_b, float scale,
+                       int32_t num_splits, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !out || !cache_len) return SPEECHKV_ERR_INVALID_ARG;
+  const int st = check_cache(cache);
+  if (st) return st;
+  if (batch < 1 || batch > kMaxGrid || num_nodes < 1 || num_nodes > SPEECHKV_MAX_TREE_NODES || max_cache_len < 0 ||
+      num_splits < 0 || num_splits > kMaxGrid)
+    return SPEECHKV_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || scale > 3.0e38f) return SPEECHKV_ERR_INVALID_ARG;  // finite, > 0
+  if ((int64_t)max_cache_len > (int64_t)cache->max_pages_per_seq * cache->page_size) return SPEECHKV_ERR_INVALID_ARG;
+  if (num_q_heads < 1 || num_q_heads % cache->num_kv_heads) return SPEECHKV_ERR_INVALID_ARG;
+  const int group = group_of(num_q_heads, cache->num_kv_heads);
+  if (group < 0) return SPEECHKV_ERR_UNSUPPORTED;
+  if (tree_mask && (mask_stride_b < 0 || mask_stride_b > ((int64_t)1 << 40))) return SPEECHKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned4(cache_len) || !aligned4(num_nodes_of) || !aligned4(tree_mask))
+    return SPEECHKV_ERR_INVALID_ARG;
+  const int32_t splits = num_splits ? num_splits
+                                    : speechkv_tree_num_splits(batch, num_nodes, num_q_heads, cache->num_kv_heads,
+                                                               max_cache_len);
+  const size_t need = speechkv_tree_workspace_bytes(batch, num_nodes, num_q_heads, cache->num_kv_heads,
+                                                    cache->head_dim, max_cache_len, splits);
+  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
+  const int words = (num_nodes + 31) / 32;
+  const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
+  const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;
+  const Region rd[] = {{q, qo}, {cache_len, lens}, {num_nodes_of, lens},
+                       {tree_mask, ((int64_t)(batch - 1) * mask_stride_b + (int64_t)num_nodes * words) * 4},
+                       {cache->block_table, table_bytes(cache, batch)}, {cache->k_pages, pool}, {cache->v_pages, pool}};
+  const Region wr[] = {{out, qo}, {need ? workspace : nullptr, (int64_t)need}};
+  if (aliased(wr, 2, rd, 7)) return SPEECHKV_ERR_ALIAS;
+  TreeArgs a;
+  a.q = q;
+  a.k_pages = cache->k_pages;
+  a.v_pages = cache->v_pages;
+  a.table = cache->block_table;
+  a.pv = view_of(cache);
+  a.cache_len = cache_len;
+  a.max_len = max_cache_len;
+  a.num_nodes = num_nodes;
+  a.nodes_of = num_nodes_of;
+  a.mask = tree_mask;
+  a.mask_stride = mask_stride_b;
+  a.mask_words = words;
+  a.num_q_heads = num_q_heads;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.num_splits = splits;
+  a.out = out;
+  a.ws_o = nullptr;
+  a.ws_ml = nullptr;
+  if (splits > 1) {
+    a.ws_o = static_cast<float*>(workspace);
+    a.ws_ml = a.ws_o + (size_t)batch * num_nodes * num_q_heads * splits * cache->head_dim;
+  }
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_tree(a, cache->dtype, cache->head_dim, group, batch, s);
+  if (e == hipSuccess && splits > 1) e = launch_tree_merge(a, cache->dtype, cache->head_dim, batch, s);
+  return status_of(e);
+}
+
+int speechkv_tree_commit(const speechkv_layer_cache* layers, int32_t num_layers, int32_t batch, const int32_t* path,
+                         int32_t max_path, const int32_t* path_len, int32_t num_nodes, void* stream) {
+  if (!layers || !path || !path_len) return SPEECHKV_ERR_INVALID_ARG;
+  if (num_layers < 1 || num_layers > SPEECHKV_MAX_COMMIT_LAYERS || batch < 1 || batch > kMaxGrid || num_nodes < 1 ||
+      num_nodes > SPEECHKV_MAX_TREE_NODES || max_path < 1 || max_path > num_nodes)
+    return SPEECHKV_ERR_INVALID_ARG;
+  if (!aligned4(path) || !aligned4(path_len)) return SPEECHKV_ERR_INVALID_ARG;
+  const speechkv_paged_kv& first = layers[0].cache;
+  const int64_t lens = (int64_t)batch * 4;
+  for (int32_t i = 0; i < num_layers; ++i) {
+    const speechkv_layer_cache& y = layers[i];
+    const int st = check_cache(&y.cache);
+    if (st) return st;
+    if (!y.cache_len || !aligned4(y.cache_len) || !aligned4(y.cache_len_out)) return SPEECHKV_ERR_INVALID_ARG;
+    if (y.cache.num_kv_heads != first.num_kv_heads || y.cache.head_dim != first.head_dim ||
+        y.cache.dtype != first.dtype)
+      return SPEECHKV_ERR_INVALID_ARG;
+  }
+  // every layer's written buffers against every layer's read ones (layers may
+  // share pools, so a K pool is checked against V pools only)
+  for (int32_t i = 0; i < num_layers; ++i) {
+    const speechkv_layer_cache& y = layers[i];
+    const int64_t pool = page_pool_bytes(&y.cache);
+    const Region paths[] = {{path, lens * max_path}, {path_len, lens}};
+    const Region own[] = {{y.cache.k_pages, pool}, {y.cache.v_pages, pool}, {y.cache_len_out, lens}};
+    if (aliased(own, 3, paths, 2)) return SPEECHKV_ERR_ALIAS;
+    for (int32_t j = 0; j < num_layers; ++j) {
+      const speechkv_layer_cache& x = layers[j];
+      const int64_t other = page_pool_bytes(&x.cache);
+      const Region rd[] = {{x.cache_len, lens}, {x.cache.block_table, table_bytes(&x.cache, batch)}};
+      if (aliased(own, 3, rd, 2)) return SPEECHKV_ERR_ALIAS;
+      if (overlaps(y.cache.k_pages, pool, x.cache.v_pages, other)) return SPEECHKV_ERR_ALIAS;
+      if (i != j && y.cache_len_out &&
+          (overlaps(y.cache_len_out, lens, x.cache.k_pages, other) ||
+           overlaps(y.cache_len_out, lens, x.cache.v_pages, other) ||
+           (x.cache_len_out && overlaps(y.cache_len_out, lens, x.cache_len_out, lens))))
+        return SPEECHKV_ERR_ALIAS;
+    }
+  }
+  CommitArgs a;
+  a.path = path;
+  a.path_len = path_len;
+  a.max_path = max_path;
+  a.num_nodes = num_nodes;
+  a.kv_heads = first.num_kv_heads;
+  for (int32_t at = 0; at < num_layers; at += kCommitLayers) {
+    const int32_t n = std::min(num_layers - at, (int32_t)kCommitLayers);
+    for (int32_t i = 0; i < n; ++i) {
+      const speechkv_layer_cache& y = layers[at + i];
+      CommitLayer& c = a.layer[i];
+      c.k_pages = y.cache.k_pages;
+      c.v_pages = y.cache.v_pages;
+      c.table = y.cache.block_table;
+      c.cache_len = y.cache_len;
+      c.cache_len_out = y.cache_len_out;
+      c.num_pages = y.cache.num_pages;
+      c.page_shift = log2_exact(y.cache.page_size);
+      c.max_pages = y.cache.max_pages_per_seq;
+    }
+    const hipError_t e = launch_commit(a, first.dtype, first.head_dim, n, batch, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return SPEECHKV_ERR_HIP;
+  }
+  return SPEECHKV_OK;
+}
+
+}  // extern "C"

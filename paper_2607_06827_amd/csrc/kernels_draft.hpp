@@ -1,0 +1,78 @@
+// Internal interface between the C-ABI host layer and the kernels of the steps
+// of several new tokens (include/speechkv_draft.h).
+#pragma once
+
+#include "kernels.hpp"
+
+namespace skv {
+
+struct AppendArgs {
+  const void* q;  // may be null
+  int64_t q_stride_b, q_stride_s, q_stride_h;  // elements
+  int num_q_heads;  // 0 without q
+  const void* k;
+  const void* v;
+  int64_t stride_b, stride_s, stride_h;
+  int num_new;
+  const int32_t* new_len;    // may be null: num_new
+  const int32_t* positions;  // null with rot = 0
+  const float* inv_freq;
+  int rot;    // rotated elements of a head
+  int pairs;  // neighbouring elements (else halves)
+  const int32_t* cache_len;
+  void* k_pages;
+  void* v_pages;
+  const int32_t* table;
+  PagedView pv;
+  void* q_out;
+  int32_t* cache_len_out;  // may be null
+};
+
+struct TreeArgs {
+  const void* q;
+  const void* k_pages;
+  const void* v_pages;
+  const int32_t* table;
+  PagedView pv;
+  const int32_t* cache_len;
+  int max_len;               // host bound on cache_len
+  int num_nodes;             // rows of q, out and the mask per sequence
+  const int32_t* nodes_of;   // may be null: num_nodes
+  const uint32_t* mask;      // null: a chain
+  int64_t mask_stride;       // words
+  int mask_words;            // words of a row
+  int num_q_heads;
+  float scale_log2;  // scale * log2(e)
+  int num_splits;
+  void* out;
+  float* ws_o;   // [B][nodes][Hq][splits][D] unnormalised partial outputs
+  float* ws_ml;  // [B][nodes][Hq][splits][2] running max (log2 units) and sum
+};
+
+// Layers of one launch of the commit kernel: their descriptions travel as
+// kernel arguments (56 bytes each, 4 KB of arguments at most).
+constexpr int kCommitLayers = 32;
+struct CommitLayer {
+  void* k_pages;
+  void* v_pages;
+  const int32_t* table;
+  const int32_t* cache_len;
+  int32_t* cache_len_out;  // may be null
+  int32_t num_pages, page_shift, max_pages;
+};
+struct CommitArgs {
+  CommitLayer layer[kCommitLayers];
+  const int32_t* path;
+  const int32_t* path_len;
+  int max_path;
+  int num_nodes;
+  int kv_heads;
+};
+
+// dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
+hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
+hipError_t launch_tree(const TreeArgs& a, int dtype, int head_dim, int group, int batch, hipStream_t s);
+hipError_t launch_tree_merge(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
+hipError_t launch_commit(const CommitArgs& a, int dtype, int head_dim, int layers, int batch, hipStream_t s);
+
+}  // namespace skv

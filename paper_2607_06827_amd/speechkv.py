@@ -1,4 +1,5 @@
-"""ctypes binding of libspeechkv.so (include/speechkv.h), same names as the C ABI.
+"""ctypes binding of libspeechkv.so (include/speechkv.h and
+include/speechkv_draft.h), same names as the C ABI.
 
 Argument marshalling only: tensors become device pointers, strides and sizes
 become integers, and a non-zero status becomes a SpeechKVError.  Every step of
@@ -38,6 +39,10 @@ MASK_WINDOW_START = 1
 MAX_WINDOW = 65536  # largest window size the pooling and attention calls take
 MAX_SEGMENTS = 1024  # most segments one sequence of a segment table may have
 NOALLOC_SCRATCH_BYTES = 16 << 20  # static split scratch of speechkv_decode_attn_noalloc, per GPU
+MAX_TREE_NODES = 1024  # most new tokens per sequence of speechkv_tree_attn and speechkv_tree_commit
+MAX_COMMIT_LAYERS = 256  # most layers of one speechkv_tree_commit
+ROPE_HALVES = 0  # elements (j, j + rot_dim / 2) of a head turn together
+ROPE_PAIRS = 1  # elements (2 j, 2 j + 1)
 
 LIBRARY_PATH = _LIB_PATH
 
@@ -62,6 +67,10 @@ class _Segments(ctypes.Structure):
                 ("max_segments", ctypes.c_int32), ("max_total_len", ctypes.c_int32)]
 
 
+class _LayerCache(ctypes.Structure):
+    _fields_ = [("cache", _PagedKV), ("cache_len", ctypes.c_void_p), ("cache_len_out", ctypes.c_void_p)]
+
+
 # The descriptions above as packed bytes, passed by address: filling a cache
 # description takes 1.0 us instead of 1.7 with a ctypes structure, and a
 # decoding step of one sequence is bound by this path.  ctypes then takes any
@@ -70,6 +79,7 @@ class _Segments(ctypes.Structure):
 _pack_paged_kv = struct.Struct("@PPPiiiiii").pack
 _pack_spans = struct.Struct("@PPPii").pack
 _pack_segments = struct.Struct("@PPPiii4x").pack  # (padded to the structure's 8-byte alignment)
+_pack_lens = struct.Struct("@PP").pack  # what follows the cache in a layer of a CacheStack
 
 
 def _int32s(*counts):
@@ -131,6 +141,18 @@ _lib.speechkv_pool_kv_bwd_segments.argtypes = [_vp, _vp, _i64, _i64, _i64, _i32,
 _lib.speechkv_pool_kv_bwd_segments.restype = ctypes.c_int
 _lib.speechkv_pool_kv_bwd_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32]
 _lib.speechkv_pool_kv_bwd_workspace_bytes.restype = _sz
+_lib.speechkv_append_kv.argtypes = [_vp, _i64, _i64, _i64, _i32, _vp, _vp, _i64, _i64, _i64, _i32, _i32, _vp,
+                                    _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.speechkv_append_kv.restype = ctypes.c_int
+_lib.speechkv_tree_attn.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _i64, _f32, _i32, _vp, _vp,
+                                    _sz, _vp]
+_lib.speechkv_tree_attn.restype = ctypes.c_int
+_lib.speechkv_tree_commit.argtypes = [_vp, _i32, _i32, _vp, _i32, _vp, _i32, _vp]
+_lib.speechkv_tree_commit.restype = ctypes.c_int
+_lib.speechkv_tree_num_splits.argtypes = [_i32] * 5
+_lib.speechkv_tree_num_splits.restype = _i32
+_lib.speechkv_tree_workspace_bytes.argtypes = [_i32] * 7
+_lib.speechkv_tree_workspace_bytes.restype = _sz
 _lib.speechkv_compressed_len.argtypes = [_i32] * 6
 _lib.speechkv_compressed_len.restype = _i64
 _lib.speechkv_decode_num_splits.argtypes = [_i32, _i32, _i32]
@@ -253,6 +275,35 @@ class Segments(_Description):
                         max([sum(t + s for t, s in x) for x in segs] or [0]))
 
 
+class CacheStack:
+    """The caches of a model's layers with their lengths, for
+    speechkv_tree_commit: caches is a list of PagedKV, cache_lens and
+    cache_lens_out are lists of device int32 [B] tensors (cache_lens_out or
+    entries of it may be None).  Made once for a set of tensors and kept beside
+    them; it keeps them alive."""
+
+    def __init__(self, caches, cache_lens, cache_lens_out=None):
+        if cache_lens_out is None:
+            cache_lens_out = [None] * len(caches)
+        if not len(caches) == len(cache_lens) == len(cache_lens_out):
+            raise ValueError("one cache_len and one cache_len_out per cache")
+        packed = []
+        self._keep = []
+        for c, n, out in zip(caches, cache_lens, cache_lens_out):
+            for x in (n,) if out is None else (n, out):
+                if x.dtype != torch.int32 or not x.is_contiguous() or x.dim() != 1:
+                    raise ValueError("cache lengths must be contiguous int32 [batch] tensors")
+                if x.shape[0] != c.block_table.shape[0]:
+                    raise ValueError("cache lengths and block tables must have one entry per sequence")
+            packed.append(c._paged_kv() + _pack_lens(n.data_ptr(), 0 if out is None else out.data_ptr()))
+            self._keep.append((c.k_pages, c.v_pages, c.block_table, n, out))
+        if len({c.block_table.shape[0] for c in caches}) > 1:
+            raise ValueError("every layer must have the same batch")
+        self.num_layers = len(caches)
+        self.batch = caches[0].block_table.shape[0] if caches else 0
+        self._packed = b"".join(packed)
+
+
 def _dtype_code(dt: torch.dtype) -> int:
     if dt == torch.bfloat16:
         return DTYPE_BF16
@@ -263,6 +314,11 @@ def _dtype_code(dt: torch.dtype) -> int:
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _int32(n) -> int:
+    """A host count of a call, -1 where int32 does not hold it (as _int32s)."""
+    return n if -2**31 <= operator.index(n) < 2**31 else -1
 
 
 def _stream(stream) -> int:
@@ -545,6 +601,137 @@ def _pool_kv_bwd(fn, name, k_raw, v_raw, s, w, gate_u, layer, l0, dk_hat, dv_hat
             dk_hat.shape[1], dk_raw.data_ptr(), dv_raw.data_ptr(), _ptr(du), _ptr(workspace), ws,
             _stream(stream))
     _check(st, name)
+
+
+def speechkv_append_kv(k: torch.Tensor, v: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
+                       positions: Optional[torch.Tensor] = None,
+                       inv_freq: Optional[torch.Tensor] = None, rope: int = ROPE_HALVES,
+                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                       new_len: Optional[torch.Tensor] = None,
+                       cache_len_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v: [B, S, Hkv, D] and q: [B, S, Hq, D] views with a contiguous last
+    axis; q_out: [B, S, Hq, D] contiguous (or q itself); positions: int32
+    [B, S]; inv_freq: fp32 [rotated elements / 2], or None: no rotation;
+    cache_len, new_len, cache_len_out: int32 [B]."""
+    shape, strides = k.shape, k.stride()
+    if shape != v.shape or strides != v.stride() or k.dtype != v.dtype:
+        raise ValueError("k and v must have one shape, one stride and one dtype")
+    if len(shape) != 4 or strides[3] != 1:
+        raise ValueError("k and v must be [B, S, Hkv, D] with a contiguous last axis")
+    B, S, Hkv, D = shape
+    qs, Hq, qp, qop = (0, 0, 0, 0), 0, None, None
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        qshape, qs = q.shape, q.stride()
+        if len(qshape) != 4 or qs[3] != 1 or qshape[0] != B or qshape[1] != S or qshape[3] != D:
+            raise ValueError("q must be [B, S, Hq, D] with a contiguous last axis")
+        if q_out.shape != qshape or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous with q's shape")
+        if q.dtype != k.dtype or q_out.dtype != k.dtype:
+            raise ValueError("q, q_out, k and v must have one dtype")
+        Hq, qp, qop = qshape[2], q.data_ptr(), q_out.data_ptr()
+    pages = cache.k_pages
+    if pages.dtype != k.dtype or pages.shape[1] != Hkv or pages.shape[3] != D or cache.block_table.shape[0] != B:
+        raise ValueError("k and v must have the cache's dtype, heads, head_dim and batch")
+    for x in (cache_len, new_len, cache_len_out):
+        if x is not None and (x.dtype != torch.int32 or x.numel() != B or not x.is_contiguous()):
+            raise ValueError("cache_len, new_len and cache_len_out must be contiguous int32 [B] tensors")
+    rot = 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous fp32 tensor")
+        if positions is None or positions.dtype != torch.int32 or positions.shape != shape[:2] or \
+                not positions.is_contiguous():
+            raise ValueError("positions must be a contiguous int32 [B, S] tensor")
+    st = _lib.speechkv_append_kv(qp, qs[0], qs[1], qs[2], Hq, k.data_ptr(), v.data_ptr(), strides[0],
+                                 strides[1], strides[2], B, S, _ptr(new_len), _ptr(positions),
+                                 _ptr(inv_freq), _int32(rot), _int32(rope), cache_len.data_ptr(), cache._paged_kv(), qop,
+                                 _ptr(cache_len_out), _stream(stream))
+    _check(st, "speechkv_append_kv")
+
+
+def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor, max_cache_len: int,
+                       out: torch.Tensor, tree_mask: Optional[torch.Tensor] = None,
+                       num_nodes: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                       num_splits: int = 0, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> None:
+    """q, out: [B, n, Hq, D] contiguous; tree_mask: int32 words of bits
+    [B, n, ceil(n/32)], or [n, ceil(n/32)] for every sequence alike (see
+    tree_mask()), or None: a chain; cache_len, num_nodes: int32 [B]."""
+    shape = q.shape
+    if len(shape) != 4 or out.shape != shape or not q.is_contiguous() or not out.is_contiguous():
+        raise ValueError("q and out must be contiguous [B, n, Hq, D] tensors of one shape")
+    B, n, Hq, D = shape
+    pages = cache.k_pages
+    if q.dtype != pages.dtype or out.dtype != pages.dtype or pages.shape[3] != D or cache.block_table.shape[0] != B:
+        raise ValueError("q and out must have the cache's dtype, head_dim and batch")
+    for x in (cache_len, num_nodes):
+        if x is not None and (x.dtype != torch.int32 or x.numel() != B or not x.is_contiguous()):
+            raise ValueError("cache_len and num_nodes must be contiguous int32 [B] tensors")
+    mask_stride = 0
+    if tree_mask is not None:
+        words = -(-n // 32)
+        if tree_mask.dtype != torch.int32 or not tree_mask.is_contiguous() or \
+                tree_mask.shape not in ((n, words), (B, n, words)):
+            raise ValueError("tree_mask must be contiguous int32 [B, n, ceil(n/32)] or [n, ceil(n/32)]")
+        mask_stride = n * words if tree_mask.dim() == 3 else 0
+    if scale is None:
+        scale = D ** -0.5
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, cache._paged_kv(), cache_len.data_ptr(),
+                                 _int32(max_cache_len), _ptr(num_nodes), _ptr(tree_mask), mask_stride, scale,
+                                 _int32(num_splits), out.data_ptr(), _ptr(workspace), ws_bytes, _stream(stream))
+    _check(st, "speechkv_tree_attn")
+
+
+def speechkv_tree_num_splits(batch: int, num_nodes: int, num_q_heads: int, num_kv_heads: int,
+                             max_cache_len: int) -> int:
+    return int(_lib.speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, max_cache_len))
+
+
+def speechkv_tree_workspace_bytes(batch: int, num_nodes: int, num_q_heads: int, num_kv_heads: int,
+                                  head_dim: int, max_cache_len: int, num_splits: int = 0) -> int:
+    return int(_lib.speechkv_tree_workspace_bytes(batch, num_nodes, num_q_heads, num_kv_heads, head_dim,
+                                                  max_cache_len, num_splits))
+
+
+def speechkv_tree_commit(layers: CacheStack, path: torch.Tensor, path_len: torch.Tensor, num_nodes: int,
+                         stream=None) -> None:
+    """path: int32 [B, max_path], path_len: int32 [B]; num_nodes: nodes per
+    sequence of the tree."""
+    if not isinstance(layers, CacheStack):
+        raise TypeError(f"{type(layers).__name__} given where the call takes a CacheStack")
+    if path.dtype != torch.int32 or path.dim() != 2 or not path.is_contiguous() or \
+            path_len.dtype != torch.int32 or not path_len.is_contiguous() or \
+            path.shape[0] != layers.batch or path_len.numel() != layers.batch:
+        raise ValueError("path and path_len must be contiguous int32 [B, max_path] and [B] tensors")
+    st = _lib.speechkv_tree_commit(layers._packed, layers.num_layers, layers.batch, path.data_ptr(),
+                                   path.shape[1], path_len.data_ptr(), _int32(num_nodes), _stream(stream))
+    _check(st, "speechkv_tree_commit")
+
+
+def tree_mask(parents, device="cuda") -> torch.Tensor:
+    """Mask words of drafted trees for speechkv_tree_attn, from each node's
+    parent: parents is one list (a tree for every sequence) or a list of lists
+    of one length, with -1 for a node without parent and every parent before
+    its children.  Node i sees itself and its ancestors."""
+    if not parents or not isinstance(parents[0], (list, tuple)):
+        return tree_mask([parents], device)[0]
+    rows = []
+    for tree in parents:
+        if len(tree) != len(parents[0]):
+            raise ValueError("trees of one batch must have one length")
+        see = []
+        for i, p in enumerate(tree):
+            if not -1 <= p < i:
+                raise ValueError("a parent must come before its children")
+            see.append((see[p] if p >= 0 else 0) | 1 << i)
+        words = -(-len(tree) // 32)
+        rows.append([[(s >> 32 * w & 0xffffffff) - (s >> 32 * w & 0x80000000) * 2 for w in range(words)]
+                     for s in see])
+    return torch.tensor(rows, dtype=torch.int32, device=device)
 
 
 def speechkv_compressed_len(prefix_len: int, speech_len: int, suffix_len: int, w: int,
