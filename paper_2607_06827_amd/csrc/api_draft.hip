@@ -107,7 +107,12 @@ int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q
   if (batch < 1 || num_nodes < 1 || num_nodes > SPEECHKV_MAX_TREE_NODES || num_kv_heads < 1 ||
       group_of(num_q_heads, num_kv_heads) < 0 || max_cache_len < 0)
     return -1;
-  return 1;
+  // (blocks of the launch: two fit a CU)
+  const int64_t blocks = (int64_t)batch * num_kv_heads * tree_row_tiles((int64_t)num_nodes * (num_q_heads / num_kv_heads));
+  const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;
+  int32_t s = 1;
+  while (blocks * s * 2 <= 512 && tiles >= 16 * s) s *= 2;
+  return s;
 }
 
 size_t speechkv_tree_workspace_bytes(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
@@ -145,6 +150,8 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   const size_t need = speechkv_tree_workspace_bytes(batch, num_nodes, num_q_heads, cache->num_kv_heads,
                                                     cache->head_dim, max_cache_len, splits);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
+  if ((int64_t)batch * cache->num_kv_heads * splits * tree_row_tiles((int64_t)num_nodes * group) > INT32_MAX)
+    return SPEECHKV_ERR_UNSUPPORTED;  // (blocks of the launch)
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;
@@ -167,8 +174,12 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   a.mask_stride = mask_stride_b;
   a.mask_words = words;
   a.num_q_heads = num_q_heads;
+  a.group_shift = log2_exact(group);
+  a.row_tiles = tree_row_tiles((int64_t)num_nodes * group);
   a.scale_log2 = scale * 1.4426950408889634f;
   a.num_splits = splits;
+  const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;
+  a.tiles_per_split = (int)((tiles + splits - 1) / splits);
   a.out = out;
   a.ws_o = nullptr;
   a.ws_ml = nullptr;
@@ -177,7 +188,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
     a.ws_ml = a.ws_o + (size_t)batch * num_nodes * num_q_heads * splits * cache->head_dim;
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_tree(a, cache->dtype, cache->head_dim, group, batch, s);
+  hipError_t e = launch_tree(a, cache->dtype, cache->head_dim, batch, s);
   if (e == hipSuccess && splits > 1) e = launch_tree_merge(a, cache->dtype, cache->head_dim, batch, s);
   return status_of(e);
 }
