@@ -150,7 +150,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   const size_t need = speechkv_tree_workspace_bytes(batch, num_nodes, num_q_heads, cache->num_kv_heads,
                                                     cache->head_dim, max_cache_len, splits);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
-  if ((int64_t)batch * cache->num_kv_heads * splits * tree_row_tiles((int64_t)num_nodes * group) > INT32_MAX)
+  if (((int64_t)batch * cache->num_kv_heads * splits + 7) * tree_row_tiles((int64_t)num_nodes * group) > INT32_MAX)
     return SPEECHKV_ERR_UNSUPPORTED;  // (blocks of the launch)
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);

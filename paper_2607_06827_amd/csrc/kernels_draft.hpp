@@ -44,6 +44,7 @@ struct TreeArgs {
   int num_q_heads;
   int group_shift;   // log2 of the query heads per KV head
   int row_tiles;     // blocks that share a (sequence, KV head)'s rows
+  int num_units;     // (sequence, KV head) pairs times splits (set by the launcher)
   float scale_log2;  // scale * log2(e)
   int num_splits;
   int tiles_per_split;  // key tiles of a split, from the host's bound
@@ -74,10 +75,10 @@ struct CommitArgs {
 
 // dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
-// Rows (nodes x heads of a group) go to blocks of 32, 64 or 128, by what they
-// fill: row groups of 32 in a block.
+// Rows (nodes x heads of a group) go to blocks of 32 or 64: row groups of 32 in
+// a block.
 constexpr int kTreeKeys = 32;  // keys of a tile
-inline int tree_row_groups(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+inline int tree_row_groups(int64_t rows) { return rows <= 32 ? 1 : 2; }
 inline int tree_row_tiles(int64_t rows) {
   const int per = 32 * tree_row_groups(rows);
   return (int)((rows + per - 1) / per);

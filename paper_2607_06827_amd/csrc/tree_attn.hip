@@ -48,6 +48,8 @@ namespace {
 constexpr float kSlack = 8.f;
 constexpr int kKeys = 32;   // keys per tile
 constexpr int kWaves = 4;
+constexpr int kMaskWords = 32;  // most words of a mask row (SPEECHKV_MAX_TREE_NODES / 32)
+constexpr int kSpreadUnits = 32;  // units from which an XCD keeps a unit's row tiles together
 
 // Layout of a K or V tile in LDS: rows of kChunks 16-byte chunks, chunk c of
 // row r at position c ^ k(r) or c ^ v(r).
@@ -66,6 +68,14 @@ struct Tile {
     return sizeof(T) == 2 ? (row % (kChunks / 4)) << 2 : ((row >> 2) & 1) << 3;
   }
 };
+
+// lds_dma16, without keeping the line in the caches.
+__device__ __forceinline__ void lds_dma16_nt(const void* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :
+               : "v"(voff), "s"(sbase), "s"(lds)
+               : "memory", "m0");
+}
 
 template <int kVm>
 __device__ __forceinline__ void wait_vm() {
@@ -178,100 +188,104 @@ __device__ __forceinline__ void add_values(uint32_t sv, const float (&p)[16], f3
   }
 }
 
-// Whether all values of a tile are finite (the same in every lane).
+// Whether all values of a tile are finite (the same in every lane): 0 times any
+// of them is 0 then, else NaN.
 template <typename T, int D>
 __device__ __forceinline__ bool all_finite(uint32_t sv, int lane) {
   typedef __attribute__((address_space(3))) const u32x4_t* lds_ptr;
-  bool bad = false;
+  uint32_t zero = 0;
+  asm volatile("" : "+v"(zero));  // (no constant: the products are to be made)
+  float sum[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < Tile<T, D>::kBytes / 1024; ++i) {
     const u32x4_t x = *(lds_ptr)(uintptr_t)(sv + 1024 * i + 16 * lane);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      bad = bad || (x[e] & 0x7f800000u) == 0x7f800000u;
-      if (sizeof(T) == 2) bad = bad || (x[e] & 0x7f80u) == 0x7f80u;
+      if constexpr (sizeof(T) == 2)
+        sum[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, (uint32_t)x[e]),
+                                                     __builtin_bit_cast(bf16x2_t, zero), sum[e & 1], false);
+      else
+        sum[e & 1] = __builtin_fmaf(__uint_as_float(x[e]), __uint_as_float(zero), sum[e & 1]);
     }
   }
-  return __builtin_amdgcn_ballot_w64(bad) == 0;
+  return __builtin_amdgcn_ballot_w64(!(sum[0] + sum[1] == 0.f)) == 0;
 }
 
-// add_values for a tile with infinities or NaN among its values, key by key: a
-// row takes the keys of its bits only.
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Infinities and NaN of a tile become 0.
 template <typename T, int D>
-__device__ __forceinline__ void add_values_by_key(uint32_t sv, const float (&p)[16], uint32_t bits,
-                                                  f32x16_t (&o)[D / 32], int lane) {
-  typedef Tile<T, D> L;
-  const int col = lane & 31, hg = lane >> 5;
+__device__ __forceinline__ void clear_non_finite(uint32_t sv, int lane) {
+  typedef __attribute__((address_space(3))) u32x4_t* lds_ptr;
 #pragma nounroll
-  for (int key = 0; key < kKeys; ++key) {
-    const int at = 4 * (key >> 3) + (key & 3);  // its element, in the lanes of half (key / 4) % 2
-    float w = p[0];
+  for (int i = 0; i < Tile<T, D>::kBytes / 1024; ++i) {
+    const lds_ptr at = (lds_ptr)(uintptr_t)(sv + 1024 * i + 16 * lane);
+    u32x4_t x = *at;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) w = i == at ? p[i] : w;
-    w = __shfl(w, col + 32 * ((key >> 2) & 1), 64);
-    const bool see = (bits >> key) & 1;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int ig = 0; ig < 4; ++ig) {
-        float v[4];
-        if constexpr (sizeof(T) == 2) {
-          typedef __attribute__((address_space(3))) const uint64_t* lds_ptr;
-          const uint64_t x = *(lds_ptr)(uintptr_t)(sv + key * L::kRowBytes + ((4 * db + ig) ^ L::v(key)) * 16 + 8 * hg);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = bf16_to_f32((uint32_t)(x >> (16 * e)) & 0xffffu);
-        } else {
-          typedef __attribute__((address_space(3))) const f32x4_t* lds_ptr;
-          const f32x4_t x = *(lds_ptr)(uintptr_t)(sv + key * L::kRowBytes + ((8 * db + 2 * ig + hg) ^ L::v(key)) * 16);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = x[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[db][4 * ig + e] += see ? w * v[e] : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 2) {
+        if (!finite(__uint_as_float(x[e] & 0xffff0000u))) x[e] &= 0xffffu;
+        if (!finite(__uint_as_float(x[e] << 16))) x[e] &= 0xffff0000u;
+      } else {
+        if (!finite(__uint_as_float(x[e]))) x[e] = 0;
       }
+    }
+    *at = x;
   }
 }
 
-// kGroups: row groups of a block (1, 2 or 4).
-template <typename T, int D, int kGroups>
-struct TreeShape {
-  static constexpr int kStreams = kWaves / kGroups;
-  static constexpr int kBuffers = kGroups;  // tile buffers of a stream
-  static constexpr int kRows = 32 * kGroups;
-  static constexpr int kTiles = kStreams * kBuffers;  // (always four)
-};
-
-template <typename T, int D, int kGroups>
+// kGroups: row groups of a block; kOnce: no other block reads its keys.
+template <typename T, int D, int kGroups, bool kOnce>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kernel(TreeArgs a) {
   typedef Tile<T, D> L;
-  typedef TreeShape<T, D, kGroups> S;
-  constexpr int kStreams = S::kStreams, kBuffers = S::kBuffers;
+  static_assert(kGroups == 1 || kGroups == 2, "row groups of a block");
+  constexpr int kStreams = kWaves / kGroups, kRows = 32 * kGroups;
   constexpr int kLoadsPerWave = L::kLoads / kGroups;
   constexpr int kVm = 2 * kLoadsPerWave;  // direct loads of a wave per tile
-  static_assert(L::kLoads % kGroups == 0 && kVm * (kBuffers > 1 ? kBuffers - 1 : 1) < 63, "vector-memory counter");
+  static_assert(L::kLoads % kGroups == 0 && kVm < 63, "vector-memory counter");
 
-  // K and V tile i at s_tile + 2 i and 2 i + 1 tiles
-  __shared__ __attribute__((aligned(1024))) unsigned char s_tile[2 * S::kTiles * L::kBytes];
+  // kGroups (K, V) buffers a stream: four of 2 kBytes
+  __shared__ __attribute__((aligned(1024))) unsigned char s_tile[4 * 2 * L::kBytes];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+  __shared__ uint32_t s_mask[kRows * kMaskWords];  // the mask rows of the block's nodes
+  __shared__ int s_far[kStreams];                  // values left out of the stream's sums (see keep_finite)
 
-  // XCD x takes a contiguous range of items, (pair, split) with their row
-  // tiles innermost: the tiles that read the same keys run side by side on one
-  // L2.
-  const int nblk = gridDim.x, per_xcd = nblk >> 3, rem = nblk & 7, xcd = blockIdx.x & 7;
-  const int item = xcd * per_xcd + min(xcd, rem) + (blockIdx.x >> 3);
-  const int row_tile = item % a.row_tiles, rest = item / a.row_tiles;
-  const int split = rest % a.num_splits, pair = rest / a.num_splits;
+  // A unit is a (sequence, KV head) and a split; its row tiles read the same
+  // keys, so they follow each other on one XCD (block index mod 8) and its L2.
+  // Units go round the XCDs, so that long sequences spread.  With few units
+  // the row tiles go round the XCDs instead.
+  const int bid = blockIdx.x, units = a.num_units;
+  int unit, row_tile;
+  if (units >= kSpreadUnits) {
+    const int at = bid >> 3;
+    unit = (at / a.row_tiles) * 8 + (bid & 7);
+    row_tile = at % a.row_tiles;
+    if (unit >= units) return;
+  } else {
+    unit = bid / a.row_tiles;
+    row_tile = bid % a.row_tiles;
+  }
+  row_tile = a.row_tiles - 1 - row_tile;  // (a chain's last rows see most keys)
+  const int split = unit % a.num_splits, pair = unit / a.num_splits;
   const int heads = a.pv.kv_heads, b = pair / heads, g = pair % heads;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % kGroups, stream = wave / kGroups;
   const int col = lane & 31, hg = lane >> 5;
   const int gshift = a.group_shift;
-  const int r = row_tile * S::kRows + rg * 32 + col;  // this lane's row
+  const int r = row_tile * kRows + rg * 32 + col;  // this lane's row
   const int node = r >> gshift;
   const int n_alloc = a.num_nodes;
 
-  // the queries first: they depend on no length
+  // this split's tiles, cut from the host's bound; step s of a stream is tile
+  // t_first + s * kStreams
+  const int t_first = split * a.tiles_per_split + stream;
+  const int shift = a.pv.page_shift, slot_mask = (1 << shift) - 1;
+
+  // What depends on no length goes out first: the queries, the block's mask
+  // rows, and the table entries of the stream's next 16 tiles (pages hold at
+  // least 8 rows, so a tile has four: lane 4 s + i has that of rows 8 i .. of
+  // step s).
   u32x4_t q[L::kFrags];
   {
     const int h = (g << gshift) + (r & ((1 << gshift) - 1));
@@ -280,25 +294,48 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
 #pragma unroll
     for (int i = 0; i < L::kFrags; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(row + 32 * i);
   }
+  const int32_t* table = a.table + (int64_t)b * a.pv.max_pages;
+  auto table_of = [&](int step) __attribute__((always_inline)) {
+    const uint32_t key = (uint32_t)(t_first + (step + (lane >> 2)) * kStreams) * kKeys + 8 * (lane & 3);
+    return table[min(key >> shift, (uint32_t)a.pv.max_pages - 1)];
+  };
+  int tbl = table_of(0);
+  const int node0 = (row_tile * kRows) >> gshift;
+  if (a.mask) {
+    const uint32_t* from = a.mask + b * a.mask_stride + (int64_t)node0 * a.mask_words;
+    const int words = min(kRows >> gshift, n_alloc - node0) * a.mask_words;
+    for (int i = tid; i < words; i += kWaves * 64) s_mask[i] = from[i];
+  }
 
-  // lengths and the first table entries come by scalar loads (no kernel writes
-  // them while this one runs)
+  if (tid < kStreams) s_far[tid] = 0;
+
+  // lengths by scalar loads (no kernel writes them while this one runs)
   typedef __attribute__((address_space(4))) const int32_t* const_ptr;
-  const int shift = a.pv.page_shift, slot_mask = (1 << shift) - 1;
   const int64_t cap = (int64_t)a.pv.max_pages << shift;
   const int nn = a.nodes_of ? min(max(((const_ptr)a.nodes_of)[b], 0), n_alloc) : n_alloc;
   const int len = (int)min((int64_t)min(max(((const_ptr)a.cache_len)[b], 0), a.max_len), cap);
-  const int node0 = (row_tile * S::kRows) >> gshift;
+  if (node0 >= nn) return;  // no node in this block
   // keys any row of the block sees: in a chain none behind its last node
-  const int node_end = a.mask ? nn : min(nn, ((row_tile * S::kRows + S::kRows - 1) >> gshift) + 1);
+  const int node_end = a.mask ? nn : min(nn, ((row_tile * kRows + kRows - 1) >> gshift) + 1);
   const int keys = (int)min((int64_t)len + node_end, cap);
   const int last = keys - 1;
   const int tiles = (keys + kKeys - 1) / kKeys;
-  // this split's tiles, cut from the host's bound
-  const int t_begin = min(split * a.tiles_per_split, tiles), t_end = min(t_begin + a.tiles_per_split, tiles);
-  const int steps = (t_end - t_begin + kStreams - 1) / kStreams;
+  const int t_end = min((split + 1) * a.tiles_per_split, tiles);
 
-  const const_ptr table = (const_ptr)(a.table + (int64_t)b * a.pv.max_pages);
+  // All of it has arrived before the first direct load, which the compiler
+  // does not count: later waits are for the direct loads alone.  A row that is
+  // no node gets zero queries: finite logits that nothing reads.
+  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+#pragma unroll
+  for (int i = 0; i < L::kFrags; ++i) {
+    if (node >= nn) q[i] = u32x4_t{0, 0, 0, 0};
+    asm volatile("" : "+v"(q[i]));
+  }
+  asm volatile("" : "+v"(tbl));
+  __builtin_amdgcn_sched_barrier(0);
+
   const uint32_t npages = (uint32_t)a.pv.num_pages;
   const uint64_t head_bytes = (uint64_t)L::kRowBytes << shift, page_bytes = head_bytes * heads;
   const uintptr_t kpool = (uintptr_t)a.k_pages + g * head_bytes;
@@ -306,39 +343,65 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
   const uint32_t lds0 = lds_addr(s_tile);
   const int lrow = lane / L::kChunks, lpos = lane % L::kChunks;  // row within a load, LDS chunk position
 
-  // Pages hold at least 8 rows: a tile has four table entries, and a load's
-  // rows lie in one page.  Keys past the last one read the last one.
+  constexpr int kShare = kKeys / kGroups;  // rows of a tile that a wave loads, from rg * kShare on
+  constexpr int kRuns = kShare / 8;        // in runs of 8, each in one page
   struct Entries {
-    int e[4];
+    uint64_t at[kRuns];  // byte offset of the run in a pool
+    uint32_t present;    // the tile's keys whose page is in range, as bits
   };
-  auto entries = [&](int t) __attribute__((always_inline)) {
+  auto entries = [&](int step) __attribute__((always_inline)) {
+    if ((step & 15) == 0 && step) {
+      tbl = table_of(step);
+      __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (here, not at every use)
+      asm volatile("" : "+v"(tbl));
+    }
+    const int t = t_first + step * kStreams;
+    const int lim = (last - t * kKeys) >> 3;  // runs past the last key read its run
     Entries x;
+    x.present = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.e[i] = table[min(t * kKeys + 8 * i, last) >> shift];
+    for (int i = 0; i < 4; ++i)
+      x.present |= (uint32_t)__builtin_amdgcn_readlane(tbl, 4 * (step & 15) + min(i, lim)) < npages ? 0xffu << (8 * i) : 0u;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) {
+      const int run = min(rg * kRuns + i, lim);
+      const uint32_t e = (uint32_t)__builtin_amdgcn_readlane(tbl, 4 * (step & 15) + run);
+      // (a bad entry reads an in-range page; its keys count as not seen)
+      x.at[i] = (uint64_t)(e < npages ? e : 0u) * page_bytes + (uint32_t)((t * kKeys + 8 * run) & slot_mask) * L::kRowBytes;
+    }
     return x;
   };
-  // keys of a tile whose page is in range, as bits
-  auto present = [&](const Entries& x) __attribute__((always_inline)) {
-    uint32_t ok = 0;
+  // This wave's share of tile t into LDS at dst (K or V).  The lane offset within
+  // a run is the same for every tile but for the swizzle of the load's first
+  // row.  In the last tile, rows past the last key read that key's row.
+  const uint32_t lane_k = lrow * L::kRowBytes + ((lpos ^ L::k(lrow)) << 4);
+  const uint32_t lane_v = lrow * L::kRowBytes + ((lpos ^ L::v(lrow)) << 4);
+  auto load = [&](int t, const Entries& x, uint32_t dst, bool is_v) __attribute__((always_inline)) {
+    const uintptr_t pool = kpool + (is_v ? v_minus_k : 0);
+    auto move = [&](uint64_t at, uint32_t off, int in) __attribute__((always_inline)) {
+      at += pool;  // (both the same in every lane, which the compiler does not always see)
+      at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(dst + (rg * kShare + in) * L::kRowBytes);
+      if constexpr (kOnce) lds_dma16_nt((const void*)at, off, to);
+      else lds_dma16((const void*)at, off, to);
+    };
+    const uint32_t k_far = rg ? L::k(kShare) << 4 : 0;
+    if (t * kKeys + kKeys <= keys) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ok |= (uint32_t)x.e[i] < npages ? 0xffu << (8 * i) : 0u;
-    return ok;
-  };
-  // this wave's share of tile t, its rows from rg * kShare on (table entries
-  // own[i] for rows 8 i.. of it), into LDS at dst (K or V)
-  constexpr int kShare = kKeys / kGroups;
-  auto load = [&](int t, const Entries& own, uint32_t dst, bool is_v) __attribute__((always_inline)) {
+      for (int i = 0; i < kLoadsPerWave; ++i) {
+        const int in = i * L::kRowsPerLoad;  // (a constant)
+        const uint32_t swz = (is_v ? L::v(in) : L::k(in)) << 4;
+        move(x.at[in / 8] + (in & 7) * L::kRowBytes, (is_v ? lane_v : lane_k ^ k_far) ^ swz, in);
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < kLoadsPerWave; ++i) {
-      const int in = i * L::kRowsPerLoad;  // (a constant)
-      const int e = own.e[in / 8];
-      const uint32_t page = (uint32_t)e < npages ? (uint32_t)e : 0u;  // a bad entry reads an in-range page
-      const uintptr_t base = kpool + (uint64_t)page * page_bytes + (is_v ? v_minus_k : 0);
-      const int row0 = rg * kShare + in, row = row0 + lrow;
-      const int key = min(t * kKeys + row, last);
-      const int swz = is_v ? L::v(row) : L::k(row);
-      lds_dma16((const void*)base, (uint32_t)((key & slot_mask) * L::kRowBytes + ((lpos ^ swz) << 4)),
-                dst + row0 * L::kRowBytes);
+      for (int i = 0; i < kLoadsPerWave; ++i) {
+        const int in = i * L::kRowsPerLoad, row = rg * kShare + in + lrow;
+        const int swz = is_v ? L::v(row) : L::k(row);
+        const int to = t * kKeys + (row | 7) > last ? min((in & 7) + lrow, last & 7) : (in & 7) + lrow;
+        move(x.at[in / 8], to * L::kRowBytes + ((lpos ^ swz) << 4), in);
+      }
     }
   };
 
@@ -349,23 +412,22 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = neg_inf(), l_run = 0.f;
 
-  // the 32 keys from kb on that this lane's row sees
-  const uint32_t* mask_row =
-      a.mask ? a.mask + b * a.mask_stride + (int64_t)min(node, n_alloc - 1) * a.mask_words : nullptr;
-  auto tile_bits = [&](int kb, uint32_t ok) __attribute__((always_inline)) -> uint32_t {
-    uint32_t bits;
+  // the 32 keys from kb on that this lane's row sees (a tile that reaches past
+  // len, or that lacks a page)
+  auto tile_bits = [&](int kb, uint32_t present) __attribute__((always_inline)) -> uint32_t {
+    uint32_t bits = ~0u;
     int lim = keys - kb;
     if (a.mask) {
-      const int j0 = kb - len, w = j0 >> 5;  // (w >= -1: the tile reaches past len)
-      const uint32_t lo = w >= 0 ? (w < a.mask_words ? mask_row[w] : 0u) : ~0u;
-      const uint32_t hi = w + 1 < a.mask_words && w + 1 >= 0 ? mask_row[w + 1] : 0u;
-      bits = w < -1 ? ~0u : (uint32_t)((((uint64_t)hi << 32) | lo) >> (j0 & 31));
+      const int j0 = kb - len, w = j0 >> 5;  // node of the first key (below 0: cached keys)
+      const uint32_t* row = s_mask + (node - node0) * a.mask_words;
+      const uint32_t lo = row[min(max(w, 0), a.mask_words - 1)], hi = row[min(max(w + 1, 0), a.mask_words - 1)];
+      if (w >= -1) bits = (uint32_t)((((uint64_t)hi << 32) | (w >= 0 ? lo : ~0u)) >> (j0 & 31));
+      // (words past the last are of nodes past the last: cut by lim)
     } else {
-      bits = ~0u;
       lim = min(lim, len + node + 1 - kb);
     }
     if (lim < 32) bits &= lim > 0 ? (1u << lim) - 1 : 0u;
-    return node < nn ? bits & ok : 0u;
+    return node < nn ? bits & present : 0u;
   };
 
   // softmax of a tile's logits: st becomes the weights
@@ -386,16 +448,16 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
       }
     }
     mt = partner_max(mt) * a.scale_log2;  // the scale is > 0
-    if (mt > m_run + kSlack) {
-      if (m_run != neg_inf()) {  // (before the first visible key o and l are still 0)
-        const float corr = fast_exp2(m_run - mt);
-        l_run *= corr;
+    // (one branch for the wave: the sums of rows that stay are multiplied by 1)
+    const bool grow = mt > m_run + kSlack;
+    if (__builtin_amdgcn_ballot_w64(grow)) {
+      const float corr = grow ? fast_exp2(m_run - mt) : 1.f;
+      l_run *= corr;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= corr;
-      }
-      m_run = mt;
+        for (int i = 0; i < 16; ++i) o[db][i] *= corr;
+      m_run = grow ? mt : m_run;
     }
     const float m_use = m_run == neg_inf() ? 0.f : m_run;
     float sum = 0.f;
@@ -407,96 +469,132 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
     l_run += sum;
   };
 
-  // A tile needs its bits where it reaches past len or lacks a page.
-  auto needs_bits = [&](int t, uint32_t ok) { return t * kKeys + kKeys > len || ok != ~0u; };
-  if (node0 >= nn) return;  // no node in this block
+  // Before the values of a tile with bits are added: those that are not finite
+  // become 0 (a row that does not see them would get 0 times infinity) and
+  // s_far says that rows that do see them are owed them.  (The flag goes up
+  // before the first value changes, so a wave that shares the tile finds the
+  // one or the other.)
+  auto keep_finite = [&](uint32_t sv) __attribute__((always_inline)) {
+    if (!all_finite<T, D>(sv, lane)) {
+      s_far[stream] = 1;
+      clear_non_finite<T, D>(sv, lane);
+      wait_lds();
+    }
+  };
 
-  // The queries have arrived, by and large, when the first table entries have.
-  // Waiting for them here, before the first direct load (which the compiler
-  // does not count), keeps later waits on the direct loads alone.  A row that
-  // is no node gets zero queries: finite logits that nothing reads.
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-#pragma unroll
-  for (int i = 0; i < L::kFrags; ++i) {
-    if (node >= nn) q[i] = u32x4_t{0, 0, 0, 0};
-    asm volatile("" : "+v"(q[i]));
-  }
-  __builtin_amdgcn_sched_barrier(0);
+  // A tile needs its bits where it reaches past len or lacks a page.
+  auto needs_bits = [&](int t, uint32_t present) { return t * kKeys + kKeys > len || present != ~0u; };
+
   if constexpr (kGroups == 1) {
     // every wave its own stream: K and V buffer of its own, no barrier
     const uint32_t sk = lds0 + wave * 2 * L::kBytes, sv = sk + L::kBytes;
-    int t = t_begin + wave;
-    if (t < t_end) {
-      Entries x = entries(t);
-      uint32_t ok = present(x);
+    if (t_first < t_end) {
+      int t = t_first, step = 0;
+      Entries x = entries(0);
       load(t, x, sk, false);
       load(t, x, sv, true);
-      if (t + kWaves < t_end) x = entries(t + kWaves);
       wait_vm<kVm / 2>();
       while (true) {
-        const bool more = t + kWaves < t_end, masked = needs_bits(t, ok);
-        uint32_t bits = masked ? tile_bits(t * kKeys, ok) : ~0u;
-        asm volatile("" : "+v"(bits));  // (loaded before the next K tile is requested)
+        const bool more = t + kStreams < t_end, masked = needs_bits(t, x.present);
+        const uint32_t bits = masked ? tile_bits(t * kKeys, x.present) : ~0u;
         const f32x16_t st = scores<T, D>(sk, q, lane);
         wait_lds();
-        if (more) load(t + kWaves, x, sk, false);
+        ++step;
+        if (more) {
+          x = entries(step);
+          load(t + kStreams, x, sk, false);
+        }
         float p[16];
         softmax(st, masked, bits, p);
         if (more) wait_vm<kVm / 2>();
         else wait_vm<0>();
-        if (masked && !all_finite<T, D>(sv, lane)) add_values_by_key<T, D>(sv, p, bits, o, lane);
-        else add_values<T, D>(sv, p, o, lane);
+        if (masked) keep_finite(sv);
+        add_values<T, D>(sv, p, o, lane);
         if (!more) break;
         wait_lds();
-        load(t + kWaves, x, sv, true);
-        ok = present(x);
-        t += kWaves;
-        if (t + kWaves < t_end) x = entries(t + kWaves);
+        t += kStreams;
+        load(t, x, sv, true);
         wait_vm<kVm / 2>();
       }
     }
   } else {
-    // tile `step` of the stream, kBuffers - 1 tiles ahead
-    const uint32_t base = lds0 + stream * kBuffers * 2 * L::kBytes;
-    auto buffer = [&](int step) { return base + (uint32_t)(step % kBuffers) * 2 * L::kBytes; };
-    auto tile_of = [&](int step) { return t_begin + step * kStreams + stream; };
-    uint32_t oks[kBuffers];  // of the tiles in flight, the next one first
-    auto request = [&](int step) __attribute__((always_inline)) -> uint32_t {
-      const int t = tile_of(step);
-      if (t >= t_end) return 0;
-      Entries own;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) own.e[i] = table[min(t * kKeys + rg * kShare + 8 * (i % (kShare / 8)), last) >> shift];
-      const Entries x = entries(t);
-      load(t, own, buffer(step), false);
-      load(t, own, buffer(step) + L::kBytes, true);
-      return present(x);
+    // two buffers a stream: a step's tile is computed while the next arrives
+    const uint32_t base = lds0 + stream * 4 * L::kBytes;
+    const int steps = (t_end - split * a.tiles_per_split + kStreams - 1) / kStreams;  // of the block
+    Entries x;
+    x.present = 0;
+    auto request = [&](int step) __attribute__((always_inline)) {
+      const int t = t_first + step * kStreams;
+      if (t >= t_end) return;
+      const uint32_t dst = base + (uint32_t)(step & 1) * 2 * L::kBytes;
+      x = entries(step);
+      load(t, x, dst, false);
+      load(t, x, dst + L::kBytes, true);
     };
-#pragma unroll
-    for (int i = 0; i < kBuffers - 1; ++i) oks[i] = i < steps ? request(i) : 0;
+    if (steps > 0) request(0);
     for (int step = 0; step < steps; ++step) {
-      // tile `step` has landed when only the tiles behind it are in flight
-      if (kBuffers > 2 && tile_of(step + kBuffers - 2) < t_end) bare_barrier<kVm * (kBuffers - 2)>();
-      else bare_barrier<0>();
-      oks[kBuffers - 1] = step + kBuffers - 1 < steps ? request(step + kBuffers - 1) : 0;
-      const int t = tile_of(step);
-      const uint32_t ok = oks[0];
+      bare_barrier<0>();  // this step's tile has landed in every wave's part
+      const int t = t_first + step * kStreams;
+      const uint32_t present = x.present;
+      request(step + 1);
       if (t < t_end) {
-        const uint32_t sk = buffer(step), sv = sk + L::kBytes;
-        const bool masked = needs_bits(t, ok);
-        const uint32_t bits = masked ? tile_bits(t * kKeys, ok) : ~0u;
+        const uint32_t sk = base + (uint32_t)(step & 1) * 2 * L::kBytes, sv = sk + L::kBytes;
+        const bool masked = needs_bits(t, present);
+        const uint32_t bits = masked ? tile_bits(t * kKeys, present) : ~0u;
         const f32x16_t st = scores<T, D>(sk, q, lane);
         float p[16];
         softmax(st, masked, bits, p);
-        if (masked && !all_finite<T, D>(sv, lane)) add_values_by_key<T, D>(sv, p, bits, o, lane);
-        else add_values<T, D>(sv, p, o, lane);
+        if (masked) keep_finite(sv);
+        add_values<T, D>(sv, p, o, lane);
       }
-#pragma unroll
-      for (int i = 0; i + 1 < kBuffers; ++i) oks[i] = oks[i + 1];
     }
   }
   __syncthreads();  // every wave is done with the tiles, and no load is in flight
+
+  // What keep_finite left out, key by key from the cache (rare: a model that
+  // has gone wrong).
+  if (s_far[stream]) {
+    const float m_use = m_run == neg_inf() ? 0.f : m_run;
+#pragma nounroll
+    for (int key = t_first * kKeys; key < min(t_end * kKeys, keys); ++key) {
+      const int t = key / kKeys;
+      if ((t - t_first) % kStreams) continue;
+      uint32_t present = 0;
+      for (int i = 0; i < 4; ++i)
+        present |= (uint32_t)table[min(t * kKeys + 8 * i, last) >> shift] < npages ? 0xffu << (8 * i) : 0u;
+      if (!needs_bits(t, present) || !(present >> (key % kKeys) & 1)) continue;
+      const bool see = tile_bits(t * kKeys, present) >> (key % kKeys) & 1;
+      const uint64_t at = (uint64_t)(uint32_t)table[key >> shift] * page_bytes + (uint64_t)(key & slot_mask) * L::kRowBytes;
+      const T* k = reinterpret_cast<const T*>(kpool + at);
+      const T* v = reinterpret_cast<const T*>(kpool + v_minus_k + at);
+      constexpr int kElems = 16 / (int)sizeof(T);  // of a chunk; this lane's are 2 i + hg
+      float z = 0.f;
+#pragma unroll
+      for (int i = 0; i < L::kFrags; ++i) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(k + (2 * i + hg) * kElems);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2)
+            z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, (uint32_t)x[e]),
+                                                __builtin_bit_cast(bf16x2_t, (uint32_t)q[i][e]), z, false);
+          else
+            z = __builtin_fmaf(__uint_as_float(x[e]), __uint_as_float(q[i][e]), z);
+        }
+      }
+      z = partner_sum(z);
+      const float w = fast_exp2(__builtin_fmaf(z, a.scale_log2, -m_use));
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const T x = v[32 * db + 8 * (i / 4) + 4 * hg + i % 4];
+          float f;
+          if constexpr (sizeof(T) == 2) f = bf16_to_f32(x);
+          else f = x;
+          if (see && !finite(f)) o[db][i] += w * f;
+        }
+    }
+  }
 
   // the waves' rows through LDS: wave w's 32 x D sums at s_o + 32 w D, 16-byte
   // chunks swizzled by the row
@@ -516,9 +614,9 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
             f32x4_t{o[db][4 * ig], o[db][4 * ig + 1], o[db][4 * ig + 2], o[db][4 * ig + 3]};
   }
   __syncthreads();
-  for (int it = tid; it < S::kRows * (D / 8); it += kWaves * 64) {
+  for (int it = tid; it < kRows * (D / 8); it += kWaves * 64) {
     const int row = it / (D / 8), ch = it % (D / 8), rr = row & 31, rw = row >> 5;
-    const int gr = row_tile * S::kRows + row, out_node = gr >> gshift;
+    const int gr = row_tile * kRows + row, out_node = gr >> gshift;
     if (out_node >= nn) continue;
     float M = neg_inf();
 #pragma unroll
@@ -558,37 +656,61 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
   }
 }
 
-// Log-sum-exp merge of the split partials of one (sequence, node, head).
+// Log-sum-exp merge of the split partials of a (sequence, node, head) row, in
+// split order: D / 4 lanes a row, four elements a lane.
+constexpr int kMergeThreads = 256;
+
 template <typename T, int D>
-__global__ __launch_bounds__(D) void tree_merge_kernel(TreeArgs a) {
-  const int b = blockIdx.z, node = blockIdx.y, h = blockIdx.x, e = threadIdx.x;
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs a) {
+  constexpr int kLanes = D / 4, kRows = kMergeThreads / kLanes;
+  const int b = blockIdx.y, e = threadIdx.x % kLanes;
+  const int in = blockIdx.x * kRows + threadIdx.x / kLanes;  // (node, head) of the sequence
   const int n = a.nodes_of ? min(a.nodes_of[b], a.num_nodes) : a.num_nodes;
-  if (node >= n) return;
+  if (in >= (int64_t)n * a.num_q_heads) return;
   const int S = a.num_splits;
-  const int64_t row = ((int64_t)b * a.num_nodes + node) * a.num_q_heads + h;
+  const int64_t row = (int64_t)b * a.num_nodes * a.num_q_heads + in;
   const float* ml = a.ws_ml + row * S * 2;
-  const float* po = a.ws_o + row * S * D + e;
+  const f32x4_t* po = reinterpret_cast<const f32x4_t*>(a.ws_o + row * S * D) + e;
+  // (the loads are unconditional, several splits at a time)
   float M = neg_inf();
+#pragma unroll 8
   for (int s = 0; s < S; ++s) M = fmaxf(M, ml[2 * s]);
-  float num = 0.f, den = 0.f;
+  const float ref = M == neg_inf() ? 0.f : M;
+  f32x4_t num = {0.f, 0.f, 0.f, 0.f};
+  float den = 0.f;
+#pragma unroll 8
   for (int s = 0; s < S; ++s) {
-    const float f = fast_exp2(ml[2 * s] - (M == neg_inf() ? 0.f : M));
-    num += f * po[(int64_t)s * D];
+    const float f = fast_exp2(ml[2 * s] - ref);
+    const f32x4_t x = po[s * kLanes];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) num[i] += f * x[i];
     den += f * ml[2 * s + 1];
   }
-  const float x = den == 0.f ? 0.f : num / den;
-  if (sizeof(T) == 2) static_cast<bf16_bits*>(a.out)[row * D + e] = (bf16_bits)f32_to_bf16(x);
-  else static_cast<float*>(a.out)[row * D + e] = x;
+  const float inv = den == 0.f ? 0.f : 1.f / den;  // (nothing seen: 0)
+  if constexpr (sizeof(T) == 2) {
+    uint2 x = make_uint2(pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv));
+    *reinterpret_cast<uint2*>(static_cast<bf16_bits*>(a.out) + row * D + 4 * e) = x;
+  } else {
+    *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + row * D + 4 * e) =
+        f32x4_t{num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+  }
 }
 
 template <typename T, int D>
 hipError_t launch_tree_d(const TreeArgs& a, int batch, hipStream_t s) {
   TreeArgs x = a;
   const int groups = tree_row_groups((int64_t)a.num_nodes << a.group_shift);
-  const dim3 grid((uint32_t)((int64_t)batch * a.pv.kv_heads * a.num_splits * a.row_tiles)), block(kWaves * 64);
-  if (groups == 1) return launch_struct(tree_kernel<T, D, 1>, grid, block, s, x);
-  if (groups == 2) return launch_struct(tree_kernel<T, D, 2>, grid, block, s, x);
-  return launch_struct(tree_kernel<T, D, 4>, grid, block, s, x);
+  x.num_units = batch * a.pv.kv_heads * a.num_splits;
+  const int64_t units = x.num_units >= kSpreadUnits ? ((int64_t)x.num_units + 7) / 8 * 8 : x.num_units;
+  const dim3 grid((uint32_t)(units * a.row_tiles)), block(kWaves * 64);
+  // one row tile: the keys are read once, past the caches (64 sequences of 862
+  // keys 47.8 -> 41.7 us, 16 of 7724 keys 103 -> 92); more tiles share them in
+  // L2 (301 nodes of 8 heads a group: 61 us, 64 without)
+  const bool once = a.row_tiles == 1;
+  if (groups == 1 && once) return launch_struct(tree_kernel<T, D, 1, true>, grid, block, s, x);
+  if (groups == 1) return launch_struct(tree_kernel<T, D, 1, false>, grid, block, s, x);
+  if (once) return launch_struct(tree_kernel<T, D, 2, true>, grid, block, s, x);
+  return launch_struct(tree_kernel<T, D, 2, false>, grid, block, s, x);
 }
 
 }  // namespace
@@ -602,14 +724,16 @@ hipError_t launch_tree(const TreeArgs& a, int dtype, int head_dim, int batch, hi
   return launch_tree_d<float, 64>(a, batch, s);
 }
 
+template <typename T, int D>
+hipError_t launch_merge_d(const TreeArgs& a, int batch, hipStream_t s) {
+  const int per = kMergeThreads / (D / 4);
+  const dim3 grid((uint32_t)(((int64_t)a.num_nodes * a.num_q_heads + per - 1) / per), batch), block(kMergeThreads);
+  return launch_struct(tree_merge_kernel<T, D>, grid, block, s, a);
+}
+
 hipError_t launch_tree_merge(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s) {
-  const dim3 grid(a.num_q_heads, a.num_nodes, batch), block(head_dim);
-  if (dtype == 1) {
-    if (head_dim == 128) return launch_struct(tree_merge_kernel<bf16_bits, 128>, grid, block, s, a);
-    return launch_struct(tree_merge_kernel<bf16_bits, 64>, grid, block, s, a);
-  }
-  if (head_dim == 128) return launch_struct(tree_merge_kernel<float, 128>, grid, block, s, a);
-  return launch_struct(tree_merge_kernel<float, 64>, grid, block, s, a);
+  if (dtype == 1) return head_dim == 128 ? launch_merge_d<bf16_bits, 128>(a, batch, s) : launch_merge_d<bf16_bits, 64>(a, batch, s);
+  return head_dim == 128 ? launch_merge_d<float, 128>(a, batch, s) : launch_merge_d<float, 64>(a, batch, s);
 }
 
 }  // namespace skv
