@@ -157,9 +157,11 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes,
                        void* stream);
 
 /* The split count speechkv_tree_attn takes for num_splits = 0 (-1 for invalid
- * arguments), and the workspace it needs (num_splits = 0: for that count). */
+ * arguments), and the workspace it needs for num_splits (0: enough for its own
+ * choice with either element type). */
 int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q_heads,
-                                 int32_t num_kv_heads, int32_t max_cache_len);
+                                 int32_t num_kv_heads, int32_t head_dim, int32_t dtype,
+                                 int32_t max_cache_len);
 size_t speechkv_tree_workspace_bytes(int32_t batch, int32_t num_nodes, int32_t num_q_heads,
                                      int32_t num_kv_heads, int32_t head_dim,
                                      int32_t max_cache_len, int32_t num_splits);

@@ -4,6 +4,7 @@
 #include "../../include/speechkv_draft.h"
 
 #include <algorithm>
+#include <cmath>
 
 #include "host_checks.hpp"
 #include "kernels_draft.hpp"
@@ -25,6 +26,69 @@ bool bad_stride(int64_t s, int64_t per16) { return s < 0 || s % per16; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int64_t table_bytes(const speechkv_paged_kv* c, int32_t batch) { return (int64_t)batch * c->max_pages_per_seq * 4; }
+
+// How speechkv_tree_attn cuts a call: row groups of a block (1, 2 or 4, of 32
+// rows each) and splits of the keys.
+struct TreePlan {
+  int groups, splits;
+};
+
+// The plan with the smallest estimated time (the given split count, if any).
+// The estimate is fitted to a sweep on MI355X over 24 shapes of 1 to 64
+// sequences, 1 to 8 KV heads, 4 to 1000 nodes and 30 to 7692 keys (bf16, 128
+// wide; the best of 1, 2 or 4 groups and of the split counts below is met
+// within 2% on average, 9% at most) and checked on 6 more of fp32 and 64-wide
+// heads (14% at most).  In us:
+//  - a launch and the first loads take 4.7, a block 1.3 and a step of one tile
+//    per stream about 1 (fp32 steps, bound by their products, 4.4 a 128-wide
+//    tile); the blocks that fit the chip run at once;
+//  - a key is read from HBM at 7 TB/s, and read again by every further row tile
+//    at a third of the cost: 64 rows of 7692 keys of 16 sequences take 89 us
+//    in one tile of 64, 108 in two of 32;
+//  - a wave's tile occupies its SIMD for 0.49;
+//  - splits cost 4.2 for the merge and the write and read of their fp32
+//    partial rows at 10 TB/s: one sequence of 7692 keys takes 71 us whole and
+//    16 in 16 splits, 64 sequences of 300 keys 19 us whole and 32 in two.
+TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, int dtype, int max_len, int splits) {
+  const bool f32 = dtype == SPEECHKV_DTYPE_F32, wide = head_dim == 128;
+  const double rows = (double)nodes * group, units = (double)batch * kv_heads, size = head_dim / 128.0;
+  const int64_t tiles = ((int64_t)max_len + nodes + kTreeKeys - 1) / kTreeKeys;
+  const double row_bytes = head_dim * (f32 ? 4.0 : 2.0);
+  const double keys_us = units * tiles * kTreeKeys * 2 * row_bytes / 7.0e6;
+  const double rows_us = units * rows * 2 * row_bytes / 7.0e6;
+  const double busy_us = f32 ? 3.5 * size : wide ? 0.49 : 0.35;
+  static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  TreePlan best = {1, splits ? splits : 1};
+  double best_us = 1e300;
+  for (int groups = 1; groups <= 4 && (groups == 1 || rows > 16 * groups); groups *= 2) {
+    const double row_tiles = tree_row_tiles((int64_t)nodes * group, groups);
+    const double step_us = f32 ? 4.4 * size : (groups == 1 ? 1.07 : groups == 2 ? 1.23 : 0.95) * (wide ? 1.0 : 0.8);
+    const double slots = 256.0 * (f32 && wide ? 1 : !f32 && !wide ? 4 : groups == 4 ? 3 : 2);
+    const double read_us = keys_us * (1 + 0.33 * (row_tiles - 1)) + rows_us;
+    const double work_us = units * row_tiles * groups * tiles * busy_us / 1024;
+    for (int i = 0; i < 10; ++i) {
+      const int s = splits ? splits : counts[i];
+      if (!splits && s > tiles) break;
+      const double steps = (double)(((tiles + s - 1) / s * groups + 3) / 4);
+      const double full = units * row_tiles * s / slots;
+      const double rounds = full >= 4 ? full + 0.5 : std::max(1.0, std::ceil(full));
+      const double us = std::max({rounds * (1.3 + step_us * steps), 1.3 + read_us, 1.3 + work_us}) +
+                        (s > 1 ? 4.2 + units * rows * s * head_dim * 16 / 10.2e6 : 0.0);
+      if (us < best_us) {
+        best_us = us;
+        best = {groups, s};
+      }
+      if (splits) break;
+    }
+  }
+  return best;
+}
+
+// Bytes of the splits' partial rows: fp32 sums, then (running maximum, weight
+// sum) pairs.
+size_t tree_partial_bytes(int32_t batch, int32_t nodes, int32_t q_heads, int32_t head_dim, int32_t splits) {
+  return splits <= 1 ? 0 : (size_t)batch * nodes * q_heads * splits * (head_dim + 2) * sizeof(float);
+}
 
 }  // namespace
 
@@ -103,27 +167,24 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s, in
 }
 
 int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
-                                 int32_t max_cache_len) {
-  if (batch < 1 || num_nodes < 1 || num_nodes > SPEECHKV_MAX_TREE_NODES || num_kv_heads < 1 ||
-      group_of(num_q_heads, num_kv_heads) < 0 || max_cache_len < 0)
+                                 int32_t head_dim, int32_t dtype, int32_t max_cache_len) {
+  if (batch < 1 || num_nodes < 1 || num_nodes > SPEECHKV_MAX_TREE_NODES || num_kv_heads < 1 || max_cache_len < 0 ||
+      (head_dim != 64 && head_dim != 128) || (dtype != SPEECHKV_DTYPE_F32 && dtype != SPEECHKV_DTYPE_BF16))
     return -1;
-  // (blocks of the launch: two fit a CU)
-  const int64_t blocks = (int64_t)batch * num_kv_heads * tree_row_tiles((int64_t)num_nodes * (num_q_heads / num_kv_heads));
-  const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;
-  int32_t s = 1;
-  while (blocks * s * 2 <= 512 && tiles >= 16 * s) s *= 2;
-  return s;
+  const int group = group_of(num_q_heads, num_kv_heads);
+  if (group < 0) return -1;
+  return tree_plan(batch, num_nodes, group, num_kv_heads, head_dim, dtype, max_cache_len, 0).splits;
 }
 
 size_t speechkv_tree_workspace_bytes(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
                                      int32_t head_dim, int32_t max_cache_len, int32_t num_splits) {
-  if (head_dim < 1 || num_splits < 0) return 0;
-  const int32_t s = speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, max_cache_len);
-  if (s < 0) return 0;
-  const size_t splits = num_splits ? num_splits : s;
-  if (splits <= 1) return 0;
-  const size_t rows = (size_t)batch * num_nodes * num_q_heads * splits;
-  return rows * head_dim * sizeof(float) + rows * 2 * sizeof(float);
+  if (num_splits < 0) return 0;
+  const int32_t f32 = speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, head_dim,
+                                               SPEECHKV_DTYPE_F32, max_cache_len);
+  const int32_t bf16 = speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, head_dim,
+                                                SPEECHKV_DTYPE_BF16, max_cache_len);
+  if (f32 < 0) return 0;
+  return tree_partial_bytes(batch, num_nodes, num_q_heads, head_dim, num_splits ? num_splits : std::max(f32, bf16));
 }
 
 int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t num_q_heads,
@@ -144,13 +205,13 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   if (tree_mask && (mask_stride_b < 0 || mask_stride_b > ((int64_t)1 << 40))) return SPEECHKV_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned4(cache_len) || !aligned4(num_nodes_of) || !aligned4(tree_mask))
     return SPEECHKV_ERR_INVALID_ARG;
-  const int32_t splits = num_splits ? num_splits
-                                    : speechkv_tree_num_splits(batch, num_nodes, num_q_heads, cache->num_kv_heads,
-                                                               max_cache_len);
-  const size_t need = speechkv_tree_workspace_bytes(batch, num_nodes, num_q_heads, cache->num_kv_heads,
-                                                    cache->head_dim, max_cache_len, splits);
+  const TreePlan plan = tree_plan(batch, num_nodes, group, cache->num_kv_heads, cache->head_dim, cache->dtype,
+                                  max_cache_len, num_splits);
+  const int32_t splits = plan.splits;
+  const size_t need = tree_partial_bytes(batch, num_nodes, num_q_heads, cache->head_dim, splits);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
-  if (((int64_t)batch * cache->num_kv_heads * splits + 7) * tree_row_tiles((int64_t)num_nodes * group) > INT32_MAX)
+  const int row_tiles = tree_row_tiles((int64_t)num_nodes * group, plan.groups);
+  if (((int64_t)batch * cache->num_kv_heads * splits + 7) * row_tiles > INT32_MAX)
     return SPEECHKV_ERR_UNSUPPORTED;  // (blocks of the launch)
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
@@ -175,7 +236,8 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   a.mask_words = words;
   a.num_q_heads = num_q_heads;
   a.group_shift = log2_exact(group);
-  a.row_tiles = tree_row_tiles((int64_t)num_nodes * group);
+  a.row_groups = plan.groups;
+  a.row_tiles = row_tiles;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.num_splits = splits;
   const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;

@@ -28,6 +28,23 @@ struct AppendArgs {
   int32_t* cache_len_out;  // may be null
 };
 
+// x / d and x % d by a multiplication, for x >= 0 and d >= 1 below 2^31: with
+// 2^(s-1) < d <= 2^s, mul = floor(2^32 (2^s - d) / d) + 1 gives x / d =
+// (mul x / 2^32 + x) / 2^s.
+struct FastDivide {
+  int32_t d, shift;
+  uint32_t mul;
+  FastDivide() = default;
+  explicit FastDivide(int32_t by) : d(by), shift(0) {
+    while (((int64_t)1 << shift) < by) ++shift;
+    mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
+  }
+  __device__ __forceinline__ void divide(int32_t x, int32_t& q, int32_t& r) const {
+    q = (int32_t)((__umulhi((uint32_t)x, mul) + (uint32_t)x) >> shift);
+    r = x - q * d;
+  }
+};
+
 struct TreeArgs {
   const void* q;
   const void* k_pages;
@@ -43,8 +60,10 @@ struct TreeArgs {
   int mask_words;            // words of a row
   int num_q_heads;
   int group_shift;   // log2 of the query heads per KV head
+  int row_groups;    // of a block: 1, 2 or 4
   int row_tiles;     // blocks that share a (sequence, KV head)'s rows
-  int num_units;     // (sequence, KV head) pairs times splits (set by the launcher)
+  int num_units;     // (sequence, KV head) pairs times splits (set by the launcher, as the divisors)
+  FastDivide by_row_tiles, by_splits, by_heads;
   float scale_log2;  // scale * log2(e)
   int num_splits;
   int tiles_per_split;  // key tiles of a split, from the host's bound
@@ -75,14 +94,10 @@ struct CommitArgs {
 
 // dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
-// Rows (nodes x heads of a group) go to blocks of 32 or 64: row groups of 32 in
-// a block.
 constexpr int kTreeKeys = 32;  // keys of a tile
-inline int tree_row_groups(int64_t rows) { return rows <= 32 ? 1 : 2; }
-inline int tree_row_tiles(int64_t rows) {
-  const int per = 32 * tree_row_groups(rows);
-  return (int)((rows + per - 1) / per);
-}
+// Blocks that the rows (nodes x heads of a group) of a (sequence, KV head) take,
+// of `groups` row groups of 32 each.
+inline int tree_row_tiles(int64_t rows, int groups) { return (int)((rows + 32 * groups - 1) / (32 * groups)); }
 hipError_t launch_tree(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
 hipError_t launch_tree_merge(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
 hipError_t launch_commit(const CommitArgs& a, int dtype, int head_dim, int layers, int batch, hipStream_t s);

@@ -236,16 +236,16 @@ __device__ __forceinline__ void clear_non_finite(uint32_t sv, int lane) {
 
 // kGroups: row groups of a block; kOnce: no other block reads its keys.
 template <typename T, int D, int kGroups, bool kOnce>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kernel(TreeArgs a) {
+__global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups == 4)) void tree_kernel(TreeArgs a) {
   typedef Tile<T, D> L;
-  static_assert(kGroups == 1 || kGroups == 2, "row groups of a block");
+  static_assert(kGroups == 1 || kGroups == 2 || kGroups == 4, "row groups of a block");
   constexpr int kStreams = kWaves / kGroups, kRows = 32 * kGroups;
   constexpr int kLoadsPerWave = L::kLoads / kGroups;
   constexpr int kVm = 2 * kLoadsPerWave;  // direct loads of a wave per tile
   static_assert(L::kLoads % kGroups == 0 && kVm < 63, "vector-memory counter");
 
-  // kGroups (K, V) buffers a stream: four of 2 kBytes
-  __shared__ __attribute__((aligned(1024))) unsigned char s_tile[4 * 2 * L::kBytes];
+  // (K, V) buffers: one a stream with one row group, else two
+  __shared__ __attribute__((aligned(1024))) unsigned char s_tile[(kGroups == 1 ? 1 : 2) * kStreams * 2 * L::kBytes];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ uint32_t s_mask[kRows * kMaskWords];  // the mask rows of the block's nodes
   __shared__ int s_far[kStreams];                  // values left out of the stream's sums (see keep_finite)
@@ -255,19 +255,24 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
   // Units go round the XCDs, so that long sequences spread.  With few units
   // the row tiles go round the XCDs instead.
   const int bid = blockIdx.x, units = a.num_units;
-  int unit, row_tile;
+  int unit, row_tile, pair, split, b, g;
   if (units >= kSpreadUnits) {
-    const int at = bid >> 3;
-    unit = (at / a.row_tiles) * 8 + (bid & 7);
-    row_tile = at % a.row_tiles;
+    a.by_row_tiles.divide(bid >> 3, unit, row_tile);
+    unit = unit * 8 + (bid & 7);
     if (unit >= units) return;
   } else {
-    unit = bid / a.row_tiles;
-    row_tile = bid % a.row_tiles;
+    a.by_row_tiles.divide(bid, unit, row_tile);
   }
   row_tile = a.row_tiles - 1 - row_tile;  // (a chain's last rows see most keys)
-  const int split = unit % a.num_splits, pair = unit / a.num_splits;
-  const int heads = a.pv.kv_heads, b = pair / heads, g = pair % heads;
+  a.by_splits.divide(unit, pair, split);
+  a.by_heads.divide(pair, b, g);
+  const int heads = a.pv.kv_heads;
+
+  // lengths by scalar loads (no kernel writes them while this one runs)
+  typedef __attribute__((address_space(4))) const int32_t* const_ptr;
+  const int n_alloc = a.num_nodes;
+  const int len_given = ((const_ptr)a.cache_len)[b];
+  const int nodes_given = a.nodes_of ? ((const_ptr)a.nodes_of)[b] : n_alloc;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % kGroups, stream = wave / kGroups;
@@ -275,7 +280,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
   const int gshift = a.group_shift;
   const int r = row_tile * kRows + rg * 32 + col;  // this lane's row
   const int node = r >> gshift;
-  const int n_alloc = a.num_nodes;
 
   // this split's tiles, cut from the host's bound; step s of a stream is tile
   // t_first + s * kStreams
@@ -300,20 +304,21 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
     return table[min(key >> shift, (uint32_t)a.pv.max_pages - 1)];
   };
   int tbl = table_of(0);
+  // (asked for by now, all of them: each would wait for the one before it if
+  // they were loaded where they are used)
+  asm volatile("" : : "s"(len_given), "s"(nodes_given), "s"(a.mask), "s"(a.mask_stride), "s"(a.mask_words),
+               "s"(a.max_len), "s"(a.k_pages), "s"(a.v_pages), "s"(a.pv.num_pages), "s"(a.tiles_per_split));
   const int node0 = (row_tile * kRows) >> gshift;
   if (a.mask) {
     const uint32_t* from = a.mask + b * a.mask_stride + (int64_t)node0 * a.mask_words;
     const int words = min(kRows >> gshift, n_alloc - node0) * a.mask_words;
     for (int i = tid; i < words; i += kWaves * 64) s_mask[i] = from[i];
   }
-
   if (tid < kStreams) s_far[tid] = 0;
 
-  // lengths by scalar loads (no kernel writes them while this one runs)
-  typedef __attribute__((address_space(4))) const int32_t* const_ptr;
   const int64_t cap = (int64_t)a.pv.max_pages << shift;
-  const int nn = a.nodes_of ? min(max(((const_ptr)a.nodes_of)[b], 0), n_alloc) : n_alloc;
-  const int len = (int)min((int64_t)min(max(((const_ptr)a.cache_len)[b], 0), a.max_len), cap);
+  const int nn = min(max(nodes_given, 0), n_alloc);
+  const int len = (int)min((int64_t)min(max(len_given, 0), a.max_len), cap);
   if (node0 >= nn) return;  // no node in this block
   // keys any row of the block sees: in a chain none behind its last node
   const int node_end = a.mask ? nn : min(nn, ((row_tile * kRows + kRows - 1) >> gshift) + 1);
@@ -386,7 +391,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
       if constexpr (kOnce) lds_dma16_nt((const void*)at, off, to);
       else lds_dma16((const void*)at, off, to);
     };
-    const uint32_t k_far = rg ? L::k(kShare) << 4 : 0;
+    const uint32_t k_far = L::k(rg * kShare) << 4;
     if (t * kKeys + kKeys <= keys) {
 #pragma unroll
       for (int i = 0; i < kLoadsPerWave; ++i) {
@@ -520,7 +525,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
   } else {
     // two buffers a stream: a step's tile is computed while the next arrives
     const uint32_t base = lds0 + stream * 4 * L::kBytes;
-    const int steps = (t_end - split * a.tiles_per_split + kStreams - 1) / kStreams;  // of the block
+    const int t_block = split * a.tiles_per_split;  // (a split behind the last key has no step)
+    const int steps = t_block < t_end ? (t_end - t_block + kStreams - 1) / kStreams : 0;
     Entries x;
     x.present = 0;
     auto request = [&](int step) __attribute__((always_inline)) {
@@ -596,12 +602,37 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void tree_kern
     }
   }
 
+  const float l_tot = partner_sum(l_run);
+  if constexpr (kStreams == 1) {
+    // every wave has its rows whole: four values of a row at a time
+    if (node >= nn) return;
+    const int64_t row = ((int64_t)b * n_alloc + node) * a.num_q_heads + (g << gshift) + (r & ((1 << gshift) - 1));
+    const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (nothing seen: 0)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int ig = 0; ig < 4; ++ig) {
+        const int e = 32 * db + 8 * ig + 4 * hg;
+        const f32x16_t& x = o[db];
+        if (a.num_splits == 1)
+          Mfma<T>::store4(static_cast<T*>(a.out) + row * D + e, x[4 * ig] * inv, x[4 * ig + 1] * inv,
+                          x[4 * ig + 2] * inv, x[4 * ig + 3] * inv);
+        else
+          Mfma<float>::store4(a.ws_o + (row * a.num_splits + split) * D + e, x[4 * ig], x[4 * ig + 1], x[4 * ig + 2],
+                              x[4 * ig + 3]);
+      }
+    if (a.num_splits > 1 && hg == 0) {
+      a.ws_ml[(row * a.num_splits + split) * 2] = m_run;
+      a.ws_ml[(row * a.num_splits + split) * 2 + 1] = l_tot;
+    }
+    return;
+  }
+
   // the waves' rows through LDS: wave w's 32 x D sums at s_o + 32 w D, 16-byte
   // chunks swizzled by the row
   float* const s_o = reinterpret_cast<float*>(s_tile);
   constexpr int kO = D / 4;  // chunks of an output row
   {
-    const float l_tot = partner_sum(l_run);
     if (hg == 0) {
       s_m[wave][col] = m_run;
       s_l[wave][col] = l_tot;
@@ -699,7 +730,10 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs a) {
 template <typename T, int D>
 hipError_t launch_tree_d(const TreeArgs& a, int batch, hipStream_t s) {
   TreeArgs x = a;
-  const int groups = tree_row_groups((int64_t)a.num_nodes << a.group_shift);
+  const int groups = a.row_groups;
+  x.by_row_tiles = FastDivide(a.row_tiles);
+  x.by_splits = FastDivide(a.num_splits);
+  x.by_heads = FastDivide(a.pv.kv_heads);
   x.num_units = batch * a.pv.kv_heads * a.num_splits;
   const int64_t units = x.num_units >= kSpreadUnits ? ((int64_t)x.num_units + 7) / 8 * 8 : x.num_units;
   const dim3 grid((uint32_t)(units * a.row_tiles)), block(kWaves * 64);
@@ -709,8 +743,10 @@ hipError_t launch_tree_d(const TreeArgs& a, int batch, hipStream_t s) {
   const bool once = a.row_tiles == 1;
   if (groups == 1 && once) return launch_struct(tree_kernel<T, D, 1, true>, grid, block, s, x);
   if (groups == 1) return launch_struct(tree_kernel<T, D, 1, false>, grid, block, s, x);
-  if (once) return launch_struct(tree_kernel<T, D, 2, true>, grid, block, s, x);
-  return launch_struct(tree_kernel<T, D, 2, false>, grid, block, s, x);
+  if (groups == 2 && once) return launch_struct(tree_kernel<T, D, 2, true>, grid, block, s, x);
+  if (groups == 2) return launch_struct(tree_kernel<T, D, 2, false>, grid, block, s, x);
+  if (once) return launch_struct(tree_kernel<T, D, 4, true>, grid, block, s, x);
+  return launch_struct(tree_kernel<T, D, 4, false>, grid, block, s, x);
 }
 
 }  // namespace

@@ -149,7 +149,7 @@ _lib.speechkv_tree_attn.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, 
 _lib.speechkv_tree_attn.restype = ctypes.c_int
 _lib.speechkv_tree_commit.argtypes = [_vp, _i32, _i32, _vp, _i32, _vp, _i32, _vp]
 _lib.speechkv_tree_commit.restype = ctypes.c_int
-_lib.speechkv_tree_num_splits.argtypes = [_i32] * 5
+_lib.speechkv_tree_num_splits.argtypes = [_i32] * 7
 _lib.speechkv_tree_num_splits.restype = _i32
 _lib.speechkv_tree_workspace_bytes.argtypes = [_i32] * 7
 _lib.speechkv_tree_workspace_bytes.restype = _sz
@@ -687,8 +687,9 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
 
 
 def speechkv_tree_num_splits(batch: int, num_nodes: int, num_q_heads: int, num_kv_heads: int,
-                             max_cache_len: int) -> int:
-    return int(_lib.speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, max_cache_len))
+                             head_dim: int, dtype: torch.dtype, max_cache_len: int) -> int:
+    return int(_lib.speechkv_tree_num_splits(batch, num_nodes, num_q_heads, num_kv_heads, head_dim,
+                                             _dtype_code(dtype), max_cache_len))
 
 
 def speechkv_tree_workspace_bytes(batch: int, num_nodes: int, num_q_heads: int, num_kv_heads: int,

@@ -63,25 +63,29 @@ def tree(q, k_pages, v_pages, table, lens, nodes, see, scale, half):
     out = np.full(q.shape, np.nan)
     bound = np.zeros(q.shape)
     for b in range(B):
-        for i in range(nodes[b]):
-            where = [slot_row(table, b, c, ps, P) for c in range(lens[b])]
-            where += [slot_row(table, b, lens[b] + j, ps, P) for j in range(nodes[b]) if see(b, i, j)]
-            where = [w for w in where if w]
-            if not where:
-                out[b, i] = 0.0
-                continue
-            pg, rw = np.array(where).T
-            for h in range(Hq):
-                K, V = k_pages[pg, h * Hkv // Hq, rw], v_pages[pg, h * Hkv // Hq, rw]
-                x = q[b, i, h]
-                z = scale * (K @ x)
-                p = np.exp(z - z.max())
-                p /= p.sum()
-                out[b, i, h] = p @ V
-                a = p @ np.abs(V)
-                e = (D + 4) * U * scale * np.max(np.abs(K) @ np.abs(x)) + 2 * U
-                weights = half if half > U else 0.0  # fp32 weights are not rounded again
-                bound[b, i, h] = half * np.abs(out[b, i, h]) + (2 * e + (len(where) + 64) * U + weights) * a
+        if nodes[b] == 0:
+            continue
+        slots = [slot_row(table, b, c, ps, P) for c in range(lens[b] + nodes[b])]
+        where = [c for c, w in enumerate(slots) if w]  # slots that have a page
+        if not where:
+            out[b, :nodes[b]] = 0.0
+            continue
+        pg, rw = np.array([slots[c] for c in where]).T
+        hide = np.array([[c >= lens[b] and not see(b, i, c - lens[b]) for c in where] for i in range(nodes[b])])
+        keys = np.sum(~hide, axis=1)[:, None]
+        for h in range(Hq):
+            K, V = k_pages[pg, h * Hkv // Hq, rw], v_pages[pg, h * Hkv // Hq, rw]
+            x = q[b, :nodes[b], h]
+            z = np.where(hide, -np.inf, scale * (x @ K.T))
+            top = z.max(1, keepdims=True)
+            p = np.exp(z - np.where(np.isinf(top), 0.0, top))
+            p /= np.where(keys, p.sum(1, keepdims=True), 1.0)
+            out[b, :nodes[b], h] = p @ V
+            a = p @ np.abs(V)
+            size = np.where(hide, 0.0, np.abs(x) @ np.abs(K).T).max(1, keepdims=True)
+            e = (D + 4) * U * scale * size + 2 * U
+            weights = half if half > U else 0.0  # fp32 weights are not rounded again
+            bound[b, :nodes[b], h] = half * np.abs(out[b, :nodes[b], h]) + (2 * e + (keys + 64) * U + weights) * a
     return out, bound * (1 + 1e-6)
 
 

@@ -140,17 +140,24 @@ def test_tree_valid_calls_reach_the_device():
 
 def test_tree_sizes():
     split, ws = skv.speechkv_tree_num_splits, skv.speechkv_tree_workspace_bytes
-    for bad in ((0, 1, 2, 2, 5), (1, 0, 2, 2, 5), (1, 1025, 2, 2, 5), (1, 1, 3, 2, 5), (1, 1, 2, 0, 5),
-                (1, 1, 2, 2, -1), (1, 1, 0, 2, 5)):
-        assert split(*bad) == -1
-        assert ws(*bad[:4], 64, bad[4]) == 0
+    BF, F32 = torch.bfloat16, torch.float32
+    for bad in ((0, 1, 2, 2, 64, 5), (1, 0, 2, 2, 64, 5), (1, 1025, 2, 2, 64, 5), (1, 1, 3, 2, 64, 5),
+                (1, 1, 2, 0, 64, 5), (1, 1, 2, 2, 64, -1), (1, 1, 0, 2, 64, 5), (1, 1, 2, 2, 32, 5)):
+        assert split(*bad[:5], BF, bad[5]) == -1
+        assert ws(*bad) == 0
+    assert split(1, 1, 2, 2, 64, torch.float16, 5) == -1
     assert ws(2, 5, 4, 2, 64, 100, -1) == 0 and ws(2, 5, 4, 2, 64, 100, 1) == 0
     for B in (1, 2, 16, 64):
         for n in (1, 8, 33, 256, 1024):
-            for L in (0, 1, 100, 2000, 7788, 65536):
-                s = split(B, n, 16, 8, L)
-                assert s >= 1 and ws(B, n, 16, 8, 128, L) == ws(B, n, 16, 8, 128, L, s)
-                assert s == 1 or ws(B, n, 16, 8, 128, L) >= B * n * 16 * s * 130 * 4
+            for D in (64, 128):
+                for L in (0, 1, 100, 2000, 7788, 65536):
+                    counts = [split(B, n, 16, 8, D, dt, L) for dt in (BF, F32)]
+                    assert all(1 <= s <= 32 and s <= (L + n + 31) // 32 for s in counts)
+                    assert ws(B, n, 16, 8, D, L) == ws(B, n, 16, 8, D, L, max(counts))
+                    for s in counts:
+                        assert s == 1 or ws(B, n, 16, 8, D, L, s) >= B * n * 16 * s * (D + 2) * 4
+    assert split(1, 8, 16, 8, 128, BF, 166) == 1 and split(64, 16, 16, 8, 128, BF, 846) == 1
+    assert split(1, 8, 16, 8, 128, BF, 7692) > 4
 
 
 # ------------------------------------------------------------------- commit

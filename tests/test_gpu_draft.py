@@ -6,7 +6,7 @@ import torch
 
 import draft_ref as ref
 from draft_ref import HALF, U, f64
-from gpu_case import guarded
+from gpu_case import guarded, launches
 from paper_2607_06827_amd import inputs
 from paper_2607_06827_amd import speechkv as skv
 
@@ -229,6 +229,55 @@ def test_tree_splits_agree(dt):
     for s in (1, 2, 3, 5, 16, 300):
         out = run_tree(cache, q, words, lens, nodes, 11, s)
         check_tree(out, cache, q, see, lens, nodes, f"{s} splits")
+
+
+SHAPES = [
+    # dtype, D, Hkv, G, B, longest, n, mask, splits, rows of a block
+    (BF, 128, 8, 2, 33, 70, 32, "tree", 1, 64),
+    (BF, 128, 8, 2, 33, 70, 32, "tree", 5, 64),
+    (BF, 128, 8, 8, 16, 90, 70, "chain", 1, 128),
+    (BF, 128, 8, 8, 16, 90, 70, "dag", 9, 128),
+    (BF, 64, 8, 2, 70, 40, 40, "dag", 1, 128),
+    (BF, 64, 8, 2, 70, 300, 32, "shared", 2, 64),
+    (F32, 128, 4, 4, 30, 30, 64, "tree", 1, 128),
+    (F32, 128, 4, 4, 24, 50, 40, "chain", 7, 128),
+    (F32, 64, 8, 2, 70, 10, 32, "tree", 1, 64),
+    (F32, 128, 8, 2, 33, 30, 32, "chain", 1, 64),
+    (F32, 64, 8, 8, 20, 20, 50, "dag", 3, 128),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_tree_block_shapes(case):
+    """Calls whose blocks hold 64 and 128 rows, with tiles of several steps,
+    splits behind the last key and values that are not finite."""
+    dt, D, Hkv, G, B, longest, n, mask, splits, rows = SHAPES[case]
+    rng = np.random.default_rng(case)
+    lens = [longest] + [int(x) for x in rng.integers(0, longest + 1, B - 1)]
+    nodes = [n] + [int(x) for x in rng.integers(0, n + 1, B - 1)]
+    cache, q, words, see, lens, nodes = tree_case((dt, D, Hkv, G, 16, lens, n, nodes, mask, 0), 700 + case)
+    out = run_tree(cache, q, words, lens, nodes, n, splits)
+    units = B * Hkv * splits
+    on_gpu, count, ws = i32(lens), i32(nodes), torch.empty(1 << 30, dtype=torch.uint8, device=DEV)
+    first = launches(lambda: skv.speechkv_tree_attn(q, cache, on_gpu, longest, out, tree_mask=words, num_nodes=count,
+                                                    num_splits=splits, workspace=ws))[0]
+    assert first == ((units + 7) // 8 * 8 * -(-n * G // rows), 256)
+    check_tree(out, cache, q, see, lens, nodes, f"case {case}")
+    # a value that is not finite in the second node: infinite where it is seen
+    at = [(b, *ref.slot_row(cache.block_table.cpu().numpy(), b, lens[b] + 1, 16, cache.v_pages.shape[0]))
+          for b in range(B) if nodes[b] > 1]
+    for b, page, row in at:
+        cache.v_pages[page, :, row, 3] = float("-inf")
+    far = run_tree(cache, q, words, lens, nodes, n, splits)
+    hit = torch.zeros(out.shape[:2], dtype=torch.bool)
+    for b, _, _ in at:
+        hit[b, :nodes[b]] = torch.tensor([bool(see(b, i, 1)) for i in range(nodes[b])])
+    assert hit.any() and torch.equal(torch.isinf(far[..., 3]).all(2).cpu(), hit)
+    for b, page, row in at:
+        cache.v_pages[page, :, row, 3] = 0.0
+    zero = run_tree(cache, q, words, lens, nodes, n, splits)
+    far[..., 3][hit.to(DEV)] = zero[..., 3][hit.to(DEV)]
+    assert torch.equal(far.nan_to_num(7.0), zero.nan_to_num(7.0))
 
 
 @pytest.mark.parametrize("dt,splits", [(BF, 1), (BF, 4), (F32, 1), (F32, 4)])
