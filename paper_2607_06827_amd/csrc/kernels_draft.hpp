@@ -6,6 +6,23 @@
 
 namespace skv {
 
+// x / d and x % d by a multiplication, for x >= 0 and d >= 1 below 2^31: with
+// 2^(s-1) < d <= 2^s, mul = floor(2^32 (2^s - d) / d) + 1 gives x / d =
+// (mul x / 2^32 + x) / 2^s.
+struct FastDivide {
+  int32_t d, shift;
+  uint32_t mul;
+  FastDivide() = default;
+  explicit FastDivide(int32_t by) : d(by), shift(0) {
+    while (((int64_t)1 << shift) < by) ++shift;
+    mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
+  }
+  __device__ __forceinline__ void divide(int32_t x, int32_t& q, int32_t& r) const {
+    q = (int32_t)((__umulhi((uint32_t)x, mul) + (uint32_t)x) >> shift);
+    r = x - q * d;
+  }
+};
+
 struct AppendArgs {
   const void* q;  // may be null
   int64_t q_stride_b, q_stride_s, q_stride_h;  // elements
@@ -26,23 +43,6 @@ struct AppendArgs {
   PagedView pv;
   void* q_out;
   int32_t* cache_len_out;  // may be null
-};
-
-// x / d and x % d by a multiplication, for x >= 0 and d >= 1 below 2^31: with
-// 2^(s-1) < d <= 2^s, mul = floor(2^32 (2^s - d) / d) + 1 gives x / d =
-// (mul x / 2^32 + x) / 2^s.
-struct FastDivide {
-  int32_t d, shift;
-  uint32_t mul;
-  FastDivide() = default;
-  explicit FastDivide(int32_t by) : d(by), shift(0) {
-    while (((int64_t)1 << shift) < by) ++shift;
-    mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
-  }
-  __device__ __forceinline__ void divide(int32_t x, int32_t& q, int32_t& r) const {
-    q = (int32_t)((__umulhi((uint32_t)x, mul) + (uint32_t)x) >> shift);
-    r = x - q * d;
-  }
 };
 
 struct TreeArgs {
@@ -75,6 +75,7 @@ struct TreeArgs {
 // Layers of one launch of the commit kernel: their descriptions travel as
 // kernel arguments (56 bytes each, 4 KB of arguments at most).
 constexpr int kCommitLayers = 32;
+constexpr int kCommitPath = 1024;  // longest path (SPEECHKV_MAX_TREE_NODES)
 struct CommitLayer {
   void* k_pages;
   void* v_pages;
@@ -90,6 +91,8 @@ struct CommitArgs {
   int max_path;
   int num_nodes;
   int kv_heads;
+  int heads, parts;    // (KV head, pool) pairs of a block, column parts of a row (set by the launcher)
+  FastDivide by_path;  // max_path (set by the launcher)
 };
 
 // dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.

@@ -181,10 +181,10 @@ class _Description:
     """What the cache and span descriptions share: each has the packing that
     the calls ask it for, and refuses the two that it is not."""
 
-    def _other_kind(self) -> bytes:
+    def _other_kind(self, *_) -> bytes:
         raise TypeError(f"{type(self).__name__} given where the call takes another description")
 
-    _paged_kv = _spans = _segments = _other_kind
+    _paged_kv = _paged_kv_for = _spans = _segments = _other_kind
 
 
 @dataclasses.dataclass
@@ -197,21 +197,29 @@ class PagedKV(_Description):
     block_table: torch.Tensor
 
     def _paged_kv(self) -> bytes:
+        return self._paged_kv_for(None)[0]
+
+    def _paged_kv_for(self, wanted):
+        """(the packed description, shape of k_pages, batch); `wanted` is the
+        element type that the call's other tensors have, if it checks that."""
         k, v, t = self.k_pages, self.v_pages, self.block_table
         if not (k.is_contiguous() and v.is_contiguous() and t.is_contiguous()):
             raise ValueError("paged cache tensors must be contiguous")
         shape, dtype = k.shape, k.dtype
         if shape != v.shape or len(shape) != 4 or dtype != v.dtype:
             raise ValueError("k_pages and v_pages must share one [pages, heads, page, dim] shape")
-        if t.dtype != torch.int32 or t.dim() != 2:
+        table = t.shape
+        if t.dtype != torch.int32 or len(table) != 2:
             raise ValueError("block_table must be int32 [batch, max_pages]")
+        if wanted is not None and dtype != wanted:
+            raise ValueError("the cache must have the dtype of the call's other tensors")
         pages, heads, page, dim = shape
         try:
-            return _pack_paged_kv(k.data_ptr(), v.data_ptr(), t.data_ptr(), pages, page, t.shape[1],
-                                  heads, dim, _dtype_code(dtype))
+            return _pack_paged_kv(k.data_ptr(), v.data_ptr(), t.data_ptr(), pages, page, table[1],
+                                  heads, dim, _dtype_code(dtype)), shape, table[0]
         except struct.error:
             return _pack_paged_kv(k.data_ptr(), v.data_ptr(), t.data_ptr(),
-                                  *_int32s(pages, page, t.shape[1], heads, dim), _dtype_code(dtype))
+                                  *_int32s(pages, page, table[1], heads, dim), _dtype_code(dtype)), shape, table[0]
 
 
 @dataclasses.dataclass
@@ -290,12 +298,12 @@ class CacheStack:
         packed = []
         self._keep = []
         for c, n, out in zip(caches, cache_lens, cache_lens_out):
+            packed.append(c._paged_kv() + _pack_lens(n.data_ptr(), 0 if out is None else out.data_ptr()))
             for x in (n,) if out is None else (n, out):
                 if x.dtype != torch.int32 or not x.is_contiguous() or x.dim() != 1:
                     raise ValueError("cache lengths must be contiguous int32 [batch] tensors")
                 if x.shape[0] != c.block_table.shape[0]:
                     raise ValueError("cache lengths and block tables must have one entry per sequence")
-            packed.append(c._paged_kv() + _pack_lens(n.data_ptr(), 0 if out is None else out.data_ptr()))
             self._keep.append((c.k_pages, c.v_pages, c.block_table, n, out))
         if len({c.block_table.shape[0] for c in caches}) > 1:
             raise ValueError("every layer must have the same batch")
@@ -613,42 +621,47 @@ def speechkv_append_kv(k: torch.Tensor, v: torch.Tensor, cache: PagedKV, cache_l
     axis; q_out: [B, S, Hq, D] contiguous (or q itself); positions: int32
     [B, S]; inv_freq: fp32 [rotated elements / 2], or None: no rotation;
     cache_len, new_len, cache_len_out: int32 [B]."""
-    shape, strides = k.shape, k.stride()
-    if shape != v.shape or strides != v.stride() or k.dtype != v.dtype:
+    shape, strides, dt, int32 = k.shape, k.stride(), k.dtype, torch.int32
+    if shape != v.shape or strides != v.stride() or dt != v.dtype:
         raise ValueError("k and v must have one shape, one stride and one dtype")
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("k and v must be [B, S, Hkv, D] with a contiguous last axis")
     B, S, Hkv, D = shape
-    qs, Hq, qp, qop = (0, 0, 0, 0), 0, None, None
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out go together")
-    if q is not None:
+    qs, Hq, qp, qop = strides, 0, None, None
+    if q is not None and q_out is not None:
         qshape, qs = q.shape, q.stride()
         if len(qshape) != 4 or qs[3] != 1 or qshape[0] != B or qshape[1] != S or qshape[3] != D:
             raise ValueError("q must be [B, S, Hq, D] with a contiguous last axis")
         if q_out.shape != qshape or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous with q's shape")
-        if q.dtype != k.dtype or q_out.dtype != k.dtype:
+        if q.dtype != dt or q_out.dtype != dt:
             raise ValueError("q, q_out, k and v must have one dtype")
         Hq, qp, qop = qshape[2], q.data_ptr(), q_out.data_ptr()
-    pages = cache.k_pages
-    if pages.dtype != k.dtype or pages.shape[1] != Hkv or pages.shape[3] != D or cache.block_table.shape[0] != B:
-        raise ValueError("k and v must have the cache's dtype, heads, head_dim and batch")
+    elif q is not q_out:
+        raise ValueError("q and q_out go together")
+    c, pages, batch = cache._paged_kv_for(dt)
+    if pages[1] != Hkv or pages[3] != D or batch != B:
+        raise ValueError("k and v must have the cache's heads, head_dim and batch")
+    lens = []
     for x in (cache_len, new_len, cache_len_out):
-        if x is not None and (x.dtype != torch.int32 or x.numel() != B or not x.is_contiguous()):
+        if x is None:
+            lens.append(None)
+        elif x.dtype != int32 or x.numel() != B or not x.is_contiguous():
             raise ValueError("cache_len, new_len and cache_len_out must be contiguous int32 [B] tensors")
-    rot = 0
+        else:
+            lens.append(x.data_ptr())
+    rot, pos, inv = 0, None, None
     if inv_freq is not None:
         rot = 2 * inv_freq.numel()
-        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq must be a contiguous fp32 tensor")
-        if positions is None or positions.dtype != torch.int32 or positions.shape != shape[:2] or \
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or rot > D:
+            raise ValueError("inv_freq must be a contiguous fp32 tensor of at most head_dim / 2 entries")
+        if positions is None or positions.dtype != int32 or positions.shape != shape[:2] or \
                 not positions.is_contiguous():
             raise ValueError("positions must be a contiguous int32 [B, S] tensor")
+        pos, inv = positions.data_ptr(), inv_freq.data_ptr()
     st = _lib.speechkv_append_kv(qp, qs[0], qs[1], qs[2], Hq, k.data_ptr(), v.data_ptr(), strides[0],
-                                 strides[1], strides[2], B, S, _ptr(new_len), _ptr(positions),
-                                 _ptr(inv_freq), _int32(rot), _int32(rope), cache_len.data_ptr(), cache._paged_kv(), qop,
-                                 _ptr(cache_len_out), _stream(stream))
+                                 strides[1], strides[2], B, S, lens[1], pos, inv, rot, _int32(rope), lens[0],
+                                 c, qop, lens[2], _stream(stream))
     _check(st, "speechkv_append_kv")
 
 
@@ -660,29 +673,36 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
     """q, out: [B, n, Hq, D] contiguous; tree_mask: int32 words of bits
     [B, n, ceil(n/32)], or [n, ceil(n/32)] for every sequence alike (see
     tree_mask()), or None: a chain; cache_len, num_nodes: int32 [B]."""
-    shape = q.shape
+    shape, dt = q.shape, q.dtype
     if len(shape) != 4 or out.shape != shape or not q.is_contiguous() or not out.is_contiguous():
         raise ValueError("q and out must be contiguous [B, n, Hq, D] tensors of one shape")
     B, n, Hq, D = shape
-    pages = cache.k_pages
-    if q.dtype != pages.dtype or out.dtype != pages.dtype or pages.shape[3] != D or cache.block_table.shape[0] != B:
+    c, pages, batch = cache._paged_kv_for(dt)
+    if out.dtype != dt or pages[3] != D or batch != B:
         raise ValueError("q and out must have the cache's dtype, head_dim and batch")
-    for x in (cache_len, num_nodes):
-        if x is not None and (x.dtype != torch.int32 or x.numel() != B or not x.is_contiguous()):
-            raise ValueError("cache_len and num_nodes must be contiguous int32 [B] tensors")
-    mask_stride = 0
+    if cache_len.dtype != torch.int32 or cache_len.numel() != B or not cache_len.is_contiguous():
+        raise ValueError("cache_len must be a contiguous int32 [B] tensor")
+    count, mask, mask_stride = None, None, 0
+    if num_nodes is not None:
+        if num_nodes.dtype != torch.int32 or num_nodes.numel() != B or not num_nodes.is_contiguous():
+            raise ValueError("num_nodes must be a contiguous int32 [B] tensor")
+        count = num_nodes.data_ptr()
     if tree_mask is not None:
-        words = -(-n // 32)
+        mshape, words = tree_mask.shape, -(-n // 32)
+        if len(mshape) == 3:
+            mask_stride = n * words
         if tree_mask.dtype != torch.int32 or not tree_mask.is_contiguous() or \
-                tree_mask.shape not in ((n, words), (B, n, words)):
+                mshape != ((B, n, words) if mask_stride else (n, words)):
             raise ValueError("tree_mask must be contiguous int32 [B, n, ceil(n/32)] or [n, ceil(n/32)]")
-        mask_stride = n * words if tree_mask.dim() == 3 else 0
+        mask = tree_mask.data_ptr()
     if scale is None:
         scale = D ** -0.5
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, cache._paged_kv(), cache_len.data_ptr(),
-                                 _int32(max_cache_len), _ptr(num_nodes), _ptr(tree_mask), mask_stride, scale,
-                                 _int32(num_splits), out.data_ptr(), _ptr(workspace), ws_bytes, _stream(stream))
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, c, cache_len.data_ptr(), _int32(max_cache_len),
+                                 count, mask, mask_stride, scale, _int32(num_splits), out.data_ptr(), ws,
+                                 ws_bytes, _stream(stream))
     _check(st, "speechkv_tree_attn")
 
 

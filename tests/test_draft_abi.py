@@ -253,6 +253,17 @@ def test_binding_refuses_tree(kw):
         skv.speechkv_tree_attn(**a)
 
 
+def test_binding_refuses_other_descriptions_for_a_cache():
+    x = host()
+    spans = skv.Spans(x["lens"], x["lens"], x["lens"], 0, 8)
+    with pytest.raises(TypeError):
+        skv.speechkv_append_kv(x["k"], x["k"].clone(), spans, x["lens"], stream=0)
+    with pytest.raises(TypeError):
+        skv.speechkv_tree_attn(x["q"], spans, x["lens"], 5, x["q"].clone(), stream=0)
+    with pytest.raises(TypeError):
+        skv.CacheStack([spans], [x["lens"]])
+
+
 def test_binding_refuses_counts_the_library_cannot_hold():
     x = host()
     for bound in (2 ** 31, 2 ** 32 + 5, -1):
