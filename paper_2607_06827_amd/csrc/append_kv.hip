@@ -8,7 +8,12 @@
 // an error of 2^-25 turns, however far the position.
 //
 // A block moves one token, a thread two 8-element chunks of a head: the two
-// whose elements turn together, or two of the elements that stay.
+// whose elements turn together, or two of the elements that stay.  Each angle's
+// sine and cosine are computed once, by a thread of their own, and shared
+// through LDS (1024 tokens of 16 + 16 heads 7.1 -> 5.5 us).  Several tokens a
+// block, or rows requested before the angles, are no faster.  Bound by HBM:
+// 12768 tokens of 16 + 16 heads take 40 us, 209 MB at 5.2 TB/s; a large copy
+// reaches 5.1.
 #include "kernels_draft.hpp"
 
 namespace skv {
@@ -17,9 +22,20 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Rows are read once.  bf16 rows leave no copy in the caches (4000 tokens of 64
+// + 16 heads: 30 us, 34 with ordinary loads); an fp32 chunk takes two loads of
+// the same lines, which costs more that way (12768 tokens of 16 + 16 heads: 89,
+// 83 with ordinary loads).
+__device__ __forceinline__ void load_row(Chunk<bf16_bits>& c, const bf16_bits* p) {
+  const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+  c.raw = make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void load_row(Chunk<float>& c, const float* p) { c.load(p); }
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   constexpr int kItems = D / 16;  // chunk pairs per head
+  __shared__ float2 s_turn[D / 2];  // (cos, sin) of the token's angles
   const int i = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int n = a.new_len ? min(max(a.new_len[b], 0), a.num_new) : a.num_new;
   const int len = max(a.cache_len[b], 0);
@@ -43,13 +59,21 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     c0 = 2 * p;
     c1 = 2 * p + 1;
   }
+  if (a.rot) {
+    if (tid < a.rot / 2) {
+      const double t = (double)a.positions[(int64_t)b * a.num_new + i] * ((double)a.inv_freq[tid] * 0.15915494309189535);
+      float s, c;
+      sincospif(2.f * (float)(t - __builtin_rint(t)), &s, &c);
+      s_turn[tid] = make_float2(c, s);
+    }
+    __syncthreads();
+  }
   float cs[8], sn[8];
   if (turns) {
-    const double pos = a.positions[(int64_t)b * a.num_new + i];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const double t = pos * ((double)a.inv_freq[8 * p + e] * 0.15915494309189535);  // turns
-      sincospif(2.f * (float)(t - __builtin_rint(t)), &sn[e], &cs[e]);
+      cs[e] = s_turn[8 * p + e].x;
+      sn[e] = s_turn[8 * p + e].y;
     }
   }
 
@@ -69,8 +93,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
             page_row<D>(page, g, (int)(slot & ((1 << a.pv.page_shift) - 1)), a.pv);
     }
     Chunk<T> x, y;
-    x.load(src + 8 * c0);
-    y.load(src + 8 * c1);
+    load_row(x, src + 8 * c0);
+    load_row(y, src + 8 * c1);
     if (turns && !is_v) {
       float u[8], w[8];
       x.to_float(u);
