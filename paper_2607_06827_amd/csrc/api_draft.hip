@@ -46,7 +46,7 @@ struct TreePlan {
 //    at a third of the cost: 64 rows of 7692 keys of 16 sequences take 89 us
 //    in one tile of 64, 108 in two of 32;
 //  - a wave's tile occupies its SIMD for 0.49;
-//  - splits cost 4.2 for the merge and the write and read of their fp32
+//  - splits cost 3.2 for the merge and the write and read of their fp32
 //    partial rows at 10 TB/s: one sequence of 7692 keys takes 71 us whole and
 //    16 in 16 splits, 64 sequences of 300 keys 19 us whole and 32 in two.
 TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, int dtype, int max_len, int splits) {
@@ -73,7 +73,7 @@ TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, 
       const double full = units * row_tiles * s / slots;
       const double rounds = full >= 4 ? full + 0.5 : std::max(1.0, std::ceil(full));
       const double us = std::max({rounds * (1.3 + step_us * steps), 1.3 + read_us, 1.3 + work_us}) +
-                        (s > 1 ? 4.2 + units * rows * s * head_dim * 16 / 10.2e6 : 0.0);
+                        (s > 1 ? 3.2 + units * rows * s * head_dim * 16 / 10.2e6 : 0.0);
       if (us < best_us) {
         best_us = us;
         best = {groups, s};

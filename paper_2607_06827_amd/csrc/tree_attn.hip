@@ -700,22 +700,40 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs a) {
   if (in >= (int64_t)n * a.num_q_heads) return;
   const int S = a.num_splits;
   const int64_t row = (int64_t)b * a.num_nodes * a.num_q_heads + in;
-  const float* ml = a.ws_ml + row * S * 2;
+  const float2* ml = reinterpret_cast<const float2*>(a.ws_ml) + row * S;
   const f32x4_t* po = reinterpret_cast<const f32x4_t*>(a.ws_o + row * S * D) + e;
-  // (the loads are unconditional, several splits at a time)
-  float M = neg_inf();
-#pragma unroll 8
-  for (int s = 0; s < S; ++s) M = fmaxf(M, ml[2 * s]);
-  const float ref = M == neg_inf() ? 0.f : M;
+  // kAtOnce splits at a time, all of their loads under way together
+  constexpr int kAtOnce = 8;
+  float M = neg_inf(), den = 0.f;
   f32x4_t num = {0.f, 0.f, 0.f, 0.f};
-  float den = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < S; ++s) {
-    const float f = fast_exp2(ml[2 * s] - ref);
-    const f32x4_t x = po[s * kLanes];
+  for (int s0 = 0; s0 < S; s0 += kAtOnce) {
+    float2 x[kAtOnce];
+    f32x4_t v[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) num[i] += f * x[i];
-    den += f * ml[2 * s + 1];
+    for (int k = 0; k < kAtOnce; ++k) {
+      x[k] = make_float2(neg_inf(), 0.f);
+      v[k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (s0 + k < S) {
+        x[k] = ml[s0 + k];
+        v[k] = po[(s0 + k) * kLanes];
+      }
+    }
+    float top = M;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, x[k].x);
+    const float ref = top == neg_inf() ? 0.f : top;
+    const float back = fast_exp2(M - ref);
+    den *= back;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) num[i] *= back;
+    M = top;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float f = fast_exp2(x[k].x - ref);
+      den += f * x[k].y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) num[i] += f * v[k][i];
+    }
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;  // (nothing seen: 0)
   if constexpr (sizeof(T) == 2) {
