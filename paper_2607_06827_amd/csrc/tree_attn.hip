@@ -196,7 +196,7 @@ __device__ __forceinline__ bool all_finite(uint32_t sv, int lane) {
   uint32_t zero = 0;
   asm volatile("" : "+v"(zero));  // (no constant: the products are to be made)
   float sum[2] = {0.f, 0.f};
-#pragma unroll
+#pragma unroll 2
   for (int i = 0; i < Tile<T, D>::kBytes / 1024; ++i) {
     const u32x4_t x = *(lds_ptr)(uintptr_t)(sv + 1024 * i + 16 * lane);
 #pragma unroll
@@ -299,11 +299,11 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
     for (int i = 0; i < L::kFrags; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(row + 32 * i);
   }
   const int32_t* table = a.table + (int64_t)b * a.pv.max_pages;
-  auto table_of = [&](int step) __attribute__((always_inline)) {
-    const uint32_t key = (uint32_t)(t_first + (step + (lane >> 2)) * kStreams) * kKeys + 8 * (lane & 3);
+  auto table_of = [&](int step, int at) __attribute__((always_inline)) {  // at: the lane
+    const uint32_t key = (uint32_t)(t_first + (step + (at >> 2)) * kStreams) * kKeys + 8 * (at & 3);
     return table[min(key >> shift, (uint32_t)a.pv.max_pages - 1)];
   };
-  int tbl = table_of(0);
+  int tbl = table_of(0, lane);
   // (asked for by now, all of them: each would wait for the one before it if
   // they were loaded where they are used)
   asm volatile("" : : "s"(len_given), "s"(nodes_given), "s"(a.mask), "s"(a.mask_stride), "s"(a.mask_words),
@@ -348,56 +348,70 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
   const uint32_t lds0 = lds_addr(s_tile);
   const int lrow = lane / L::kChunks, lpos = lane % L::kChunks;  // row within a load, LDS chunk position
 
+  // A run is 8 rows of a tile, all in one page.  Sixteen steps at a time, lane
+  // 4 s + i works out where run i of step s starts in the K pool (run_at) and
+  // whether its page is in range (run_ok).  Runs past the last key take its run's
+  // place, runs without a page that of page 0: rows that exist, of keys that
+  // count as not seen.
   constexpr int kShare = kKeys / kGroups;  // rows of a tile that a wave loads, from rg * kShare on
-  constexpr int kRuns = kShare / 8;        // in runs of 8, each in one page
+  constexpr int kRuns = kShare / 8;
+  uint32_t run_lo = 0, run_hi = 0;
+  uint64_t run_ok = 0;
+  auto place_runs = [&](int step, int entry, int at) __attribute__((always_inline)) {
+    const int kb = (t_first + (step + (at >> 2)) * kStreams) * kKeys;
+    const int run = min(at & 3, max((last - kb) >> 3, 0));
+    const uint32_t e = (uint32_t)__shfl(entry, (at & ~3) + run, 64);
+    const uint64_t start = kpool + (uint64_t)(e < npages ? e : 0u) * page_bytes +
+                           (uint32_t)((kb + 8 * run) & slot_mask) * L::kRowBytes;
+    run_lo = (uint32_t)start;
+    run_hi = (uint32_t)(start >> 32);
+    run_ok = __builtin_amdgcn_ballot_w64(e < npages);
+  };
+  place_runs(0, tbl, lane);
   struct Entries {
-    uint64_t at[kRuns];  // byte offset of the run in a pool
+    uint64_t at[kRuns];  // where the runs that this wave loads start in the K pool
     uint32_t present;    // the tile's keys whose page is in range, as bits
   };
   auto entries = [&](int step) __attribute__((always_inline)) {
-    if ((step & 15) == 0 && step) {
-      tbl = table_of(step);
+    const int lane0 = 4 * (step & 15);
+    if (lane0 == 0 && step) {
+      int at = lane;
+      asm volatile("" : "+v"(at));  // (nothing of this is kept in registers meanwhile)
+      const int entry = table_of(step, at);
       __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);  // (here, not at every use)
-      asm volatile("" : "+v"(tbl));
+      place_runs(step, entry, at);
+      asm volatile("" : "+v"(run_lo), "+v"(run_hi));
     }
-    const int t = t_first + step * kStreams;
-    const int lim = (last - t * kKeys) >> 3;  // runs past the last key read its run
     Entries x;
-    x.present = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      x.present |= (uint32_t)__builtin_amdgcn_readlane(tbl, 4 * (step & 15) + min(i, lim)) < npages ? 0xffu << (8 * i) : 0u;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int run = min(rg * kRuns + i, lim);
-      const uint32_t e = (uint32_t)__builtin_amdgcn_readlane(tbl, 4 * (step & 15) + run);
-      // (a bad entry reads an in-range page; its keys count as not seen)
-      x.at[i] = (uint64_t)(e < npages ? e : 0u) * page_bytes + (uint32_t)((t * kKeys + 8 * run) & slot_mask) * L::kRowBytes;
+      const int from = lane0 + rg * kRuns + i;
+      x.at[i] = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(run_hi, from) << 32 |
+                (uint32_t)__builtin_amdgcn_readlane(run_lo, from);
     }
+    const uint32_t ok = (uint32_t)(run_ok >> lane0) & 15u;
+    x.present = ((ok * 0x00204081u) & 0x01010101u) * 0xffu;  // each bit to a byte
     return x;
   };
-  // This wave's share of tile t into LDS at dst (K or V).  The lane offset within
-  // a run is the same for every tile but for the swizzle of the load's first
-  // row.  In the last tile, rows past the last key read that key's row.
-  const uint32_t lane_k = lrow * L::kRowBytes + ((lpos ^ L::k(lrow)) << 4);
+  // This wave's share of tile t into LDS at dst (K or V).  The lane offset of a
+  // load within its run is the same for every tile.  In the last tile, rows past
+  // the last key read that key's row.
+  const uint32_t lane_k = lrow * L::kRowBytes + ((lpos ^ L::k(lrow) ^ L::k(rg * kShare)) << 4);
   const uint32_t lane_v = lrow * L::kRowBytes + ((lpos ^ L::v(lrow)) << 4);
   auto load = [&](int t, const Entries& x, uint32_t dst, bool is_v) __attribute__((always_inline)) {
-    const uintptr_t pool = kpool + (is_v ? v_minus_k : 0);
     auto move = [&](uint64_t at, uint32_t off, int in) __attribute__((always_inline)) {
-      at += pool;  // (both the same in every lane, which the compiler does not always see)
-      at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
-           (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+      if (is_v) at += v_minus_k;
+      // (the same in every lane, which the compiler does not always see)
       const uint32_t to = __builtin_amdgcn_readfirstlane(dst + (rg * kShare + in) * L::kRowBytes);
       if constexpr (kOnce) lds_dma16_nt((const void*)at, off, to);
       else lds_dma16((const void*)at, off, to);
     };
-    const uint32_t k_far = L::k(rg * kShare) << 4;
     if (t * kKeys + kKeys <= keys) {
 #pragma unroll
       for (int i = 0; i < kLoadsPerWave; ++i) {
         const int in = i * L::kRowsPerLoad;  // (a constant)
         const uint32_t swz = (is_v ? L::v(in) : L::k(in)) << 4;
-        move(x.at[in / 8] + (in & 7) * L::kRowBytes, (is_v ? lane_v : lane_k ^ k_far) ^ swz, in);
+        move(x.at[in / 8], ((is_v ? lane_v : lane_k) ^ swz) + (in & 7) * L::kRowBytes, in);
       }
     } else {
 #pragma unroll
@@ -605,14 +619,18 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
   const float l_tot = partner_sum(l_run);
   if constexpr (kStreams == 1) {
     // every wave has its rows whole: four values of a row at a time
-    if (node >= nn) return;
-    const int64_t row = ((int64_t)b * n_alloc + node) * a.num_q_heads + (g << gshift) + (r & ((1 << gshift) - 1));
+    int at = lane;
+    asm volatile("" : "+v"(at));  // (the row's number is worked out again, not kept through the loop)
+    const int mine = row_tile * kRows + rg * 32 + (at & 31), half = at >> 5;
+    if ((mine >> gshift) >= nn) return;
+    const int64_t row = ((int64_t)b * n_alloc + (mine >> gshift)) * a.num_q_heads + (g << gshift) +
+                        (mine & ((1 << gshift) - 1));
     const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (nothing seen: 0)
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int ig = 0; ig < 4; ++ig) {
-        const int e = 32 * db + 8 * ig + 4 * hg;
+        const int e = 32 * db + 8 * ig + 4 * half;
         const f32x16_t& x = o[db];
         if (a.num_splits == 1)
           Mfma<T>::store4(static_cast<T*>(a.out) + row * D + e, x[4 * ig] * inv, x[4 * ig + 1] * inv,
@@ -621,7 +639,7 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
           Mfma<float>::store4(a.ws_o + (row * a.num_splits + split) * D + e, x[4 * ig], x[4 * ig + 1], x[4 * ig + 2],
                               x[4 * ig + 3]);
       }
-    if (a.num_splits > 1 && hg == 0) {
+    if (a.num_splits > 1 && half == 0) {
       a.ws_ml[(row * a.num_splits + split) * 2] = m_run;
       a.ws_ml[(row * a.num_splits + split) * 2 + 1] = l_tot;
     }
