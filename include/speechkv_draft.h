@@ -74,7 +74,7 @@ extern "C" {
  * k, v           device, as q with num_kv_heads heads and the strides
  *                stride_b, stride_s, stride_h.
  * batch          sequences (1 .. 65535).
- * num_new        new tokens per sequence in q, k, v and q_out (>= 1).
+ * num_new        new tokens per sequence in q, k, v and q_out (1 .. 2^24 - 1).
  * new_len        device int32 [batch], how many of them sequence b has (0 ..
  *                num_new), or NULL: all.  The rows behind them are neither
  *                read nor written.
@@ -140,7 +140,8 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s,
  * scale          logit scale, finite and > 0.
  * num_splits     key ranges each (sequence, KV head) is split into; 0 selects
  *                speechkv_tree_num_splits().  Partial results are merged in a
- *                fixed order: the same call gives the same bits.
+ *                fixed order: the same call gives the same bits.  UNSUPPORTED
+ *                where the launch would need 2^24 blocks or more.
  * workspace      device scratch of at least speechkv_tree_workspace_bytes(...)
  *                bytes (16-byte aligned; any contents); may be NULL when that
  *                size is 0.  Calls that overlap in time need one each.

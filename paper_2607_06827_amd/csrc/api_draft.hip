@@ -13,6 +13,10 @@ namespace {
 
 using namespace skv;
 
+// Most blocks of 256 threads along one axis of a launch (its threads are counted
+// in 32 bits).
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+
 // Bytes from the first to past the last element of a strided [batch][rows]
 // [heads][dim] tensor, or -1 when they do not fit 2^62 (no tensor is so long).
 int64_t extent(int64_t batch, int64_t sb, int64_t rows, int64_t ss, int64_t heads, int64_t sh, int64_t dim,
@@ -103,7 +107,7 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s, in
   if (!k || !v || !cache_len || (q == nullptr) != (q_out == nullptr)) return SPEECHKV_ERR_INVALID_ARG;
   const int st = check_cache(cache);
   if (st) return st;
-  if (batch < 1 || batch > kMaxGrid || num_new < 1) return SPEECHKV_ERR_INVALID_ARG;
+  if (batch < 1 || batch > kMaxGrid || num_new < 1 || num_new > kMaxBlocks) return SPEECHKV_ERR_INVALID_ARG;
   if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return SPEECHKV_ERR_INVALID_ARG;
   if (rope != SPEECHKV_ROPE_HALVES && rope != SPEECHKV_ROPE_PAIRS) return SPEECHKV_ERR_INVALID_ARG;
   if (rot_dim && (!positions || !inv_freq)) return SPEECHKV_ERR_INVALID_ARG;
@@ -211,8 +215,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   const size_t need = tree_partial_bytes(batch, num_nodes, num_q_heads, cache->head_dim, splits);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
   const int row_tiles = tree_row_tiles((int64_t)num_nodes * group, plan.groups);
-  if (((int64_t)batch * cache->num_kv_heads * splits + 7) * row_tiles > INT32_MAX)
-    return SPEECHKV_ERR_UNSUPPORTED;  // (blocks of the launch)
+  if (((int64_t)batch * cache->num_kv_heads * splits + 7) * row_tiles > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;

@@ -69,7 +69,7 @@ def append(c=None, **kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(k=None), E_ARG), (dict(v=None), E_ARG), (dict(clen=None), E_ARG), (dict(q=None), E_ARG),
     (dict(q_out=None), E_ARG), (dict(batch=0), E_ARG), (dict(batch=65536), E_ARG), (dict(n=0), E_ARG),
-    (dict(rot=-16), E_ARG), (dict(rot=80), E_ARG), (dict(rot=24), E_ARG), (dict(rope=2), E_ARG),
+    (dict(n=1 << 24), E_ARG), (dict(rot=-16), E_ARG), (dict(rot=80), E_ARG), (dict(rot=24), E_ARG), (dict(rope=2), E_ARG),
     (dict(rope=-1), E_ARG), (dict(pos=None), E_ARG), (dict(inv=None), E_ARG), (dict(hq=3), E_ARG),
     (dict(hq=0), E_ARG), (dict(hq=6), E_UNS), (dict(sb=4), E_ARG), (dict(ss=-8), E_ARG), (dict(qsh=12), E_ARG),
     (dict(k=at(9) + 8), E_ARG), (dict(q=at(8) + 4), E_ARG), (dict(q_out=at(14) + 8), E_ARG),
@@ -136,6 +136,12 @@ def test_tree_valid_calls_reach_the_device():
     assert need > 0 and tree(splits=3, ws=at(13), ws_bytes=need) == E_HIP
     assert tree(splits=3, ws=at(13), ws_bytes=need - 1) == E_WS
     assert tree(max_len=128) == E_HIP and tree(max_len=0) == E_HIP
+
+
+def test_tree_rejects_an_oversized_grid():
+    huge = dict(batch=1000, splits=65535, ws=at(64), ws_bytes=1 << 46, q=1 << 50, out=1 << 51, mask=None)
+    assert tree(**huge) == E_UNS
+    assert tree(**dict(huge, splits=8000)) == E_HIP  # (2 x 1000 x 8000 blocks: the ranges do not meet)
 
 
 def test_tree_sizes():

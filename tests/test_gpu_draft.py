@@ -151,6 +151,10 @@ TREE = [
     (BF, 128, 1, 8, 32, [45, 300], 70, [61, 70], "chain", 0),
     (BF, 128, 1, 2, 16, [1500], 65, None, "tree", 7),
     (BF, 128, 1, 2, 128, [700, 20], 64, None, "dag", 5),
+    (BF, 128, 3, 2, 16, [40, 111, 3, 64], 7, [7, 2, 7, 1], "tree", 1),
+    (BF, 64, 5, 4, 16, [0, 2, 600], 50, [50, 1, 0], "tree", 3),
+    (BF, 128, 1, 1, 16, [90], 1024, None, "chain", 0),
+    (BF, 64, 1, 1, 8, [3], 1024, [1000], "tree", 2),
     (F32, 64, 2, 2, 16, [166, 0, 5], 8, [8, 8, 2], "tree", 0),
     (F32, 128, 1, 4, 8, [33, 1, 90], 33, [1, 33, 20], "dag", 1),
     (F32, 128, 2, 1, 32, [500], 21, None, "chain", 4),
