@@ -29,6 +29,35 @@ bool bad_stride(int64_t s, int64_t per16) { return s < 0 || s % per16; }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+// Whether a region of one list overlaps a region of another (null ones take no
+// part).  Lists that lie apart as a whole, as pools and lengths mostly do, are
+// not compared pair by pair.
+template <typename A, typename B>
+bool meet(int na, const A& a, int nb, const B& b) {
+  uintptr_t a_lo = UINTPTR_MAX, a_hi = 0, b_lo = UINTPTR_MAX, b_hi = 0;
+  for (int i = 0; i < na; ++i) {
+    const Region x = a(i);
+    if (!x.p) continue;
+    a_lo = std::min(a_lo, (uintptr_t)x.p);
+    a_hi = std::max(a_hi, (uintptr_t)x.p + (uintptr_t)x.n);
+  }
+  for (int i = 0; i < nb; ++i) {
+    const Region x = b(i);
+    if (!x.p) continue;
+    b_lo = std::min(b_lo, (uintptr_t)x.p);
+    b_hi = std::max(b_hi, (uintptr_t)x.p + (uintptr_t)x.n);
+  }
+  if (a_hi <= b_lo || b_hi <= a_lo) return false;
+  for (int i = 0; i < na; ++i) {
+    const Region x = a(i);
+    for (int j = 0; x.p && j < nb; ++j) {
+      const Region y = b(j);
+      if (y.p && overlaps(x.p, x.n, y.p, y.n)) return true;
+    }
+  }
+  return false;
+}
+
 int64_t table_bytes(const speechkv_paged_kv* c, int32_t batch) { return (int64_t)batch * c->max_pages_per_seq * 4; }
 
 // How speechkv_tree_attn cuts a call: row groups of a block (1, 2 or 4, of 32
@@ -276,27 +305,23 @@ int speechkv_tree_commit(const speechkv_layer_cache* layers, int32_t num_layers,
         y.cache.dtype != first.dtype)
       return SPEECHKV_ERR_INVALID_ARG;
   }
-  // every layer's written buffers against every layer's read ones (layers may
-  // share pools, so a K pool is checked against V pools only)
-  for (int32_t i = 0; i < num_layers; ++i) {
-    const speechkv_layer_cache& y = layers[i];
-    const int64_t pool = page_pool_bytes(&y.cache);
-    const Region paths[] = {{path, lens * max_path}, {path_len, lens}};
-    const Region own[] = {{y.cache.k_pages, pool}, {y.cache.v_pages, pool}, {y.cache_len_out, lens}};
-    if (aliased(own, 3, paths, 2)) return SPEECHKV_ERR_ALIAS;
-    for (int32_t j = 0; j < num_layers; ++j) {
-      const speechkv_layer_cache& x = layers[j];
-      const int64_t other = page_pool_bytes(&x.cache);
-      const Region rd[] = {{x.cache_len, lens}, {x.cache.block_table, table_bytes(&x.cache, batch)}};
-      if (aliased(own, 3, rd, 2)) return SPEECHKV_ERR_ALIAS;
-      if (overlaps(y.cache.k_pages, pool, x.cache.v_pages, other)) return SPEECHKV_ERR_ALIAS;
-      if (i != j && y.cache_len_out &&
-          (overlaps(y.cache_len_out, lens, x.cache.k_pages, other) ||
-           overlaps(y.cache_len_out, lens, x.cache.v_pages, other) ||
-           (x.cache_len_out && overlaps(y.cache_len_out, lens, x.cache_len_out, lens))))
-        return SPEECHKV_ERR_ALIAS;
-    }
-  }
+  // every layer's written buffers against every layer's read ones and against the
+  // other written ones (layers may share pools, so K pools are checked against V
+  // pools only)
+  auto k_pool = [&](int i) { return Region{layers[i].cache.k_pages, page_pool_bytes(&layers[i].cache)}; };
+  auto v_pool = [&](int i) { return Region{layers[i].cache.v_pages, page_pool_bytes(&layers[i].cache)}; };
+  auto out = [&](int i) { return Region{layers[i].cache_len_out, lens}; };
+  auto len = [&](int i) { return Region{layers[i].cache_len, lens}; };
+  auto table = [&](int i) { return Region{layers[i].cache.block_table, table_bytes(&layers[i].cache, batch)}; };
+  auto paths = [&](int i) { return i ? Region{path_len, lens} : Region{path, lens * max_path}; };
+  const int n = num_layers;
+  if (meet(n, k_pool, n, v_pool) || meet(n, k_pool, n, out) || meet(n, v_pool, n, out) || meet(n, k_pool, n, len) ||
+      meet(n, v_pool, n, len) || meet(n, out, n, len) || meet(n, k_pool, n, table) || meet(n, v_pool, n, table) ||
+      meet(n, out, n, table) || meet(n, k_pool, 2, paths) || meet(n, v_pool, 2, paths) || meet(n, out, 2, paths))
+    return SPEECHKV_ERR_ALIAS;
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (out(i).p && out(j).p && overlaps(out(i).p, lens, out(j).p, lens)) return SPEECHKV_ERR_ALIAS;
   CommitArgs a;
   a.path = path;
   a.path_len = path_len;
@@ -304,8 +329,8 @@ int speechkv_tree_commit(const speechkv_layer_cache* layers, int32_t num_layers,
   a.num_nodes = num_nodes;
   a.kv_heads = first.num_kv_heads;
   for (int32_t at = 0; at < num_layers; at += kCommitLayers) {
-    const int32_t n = std::min(num_layers - at, (int32_t)kCommitLayers);
-    for (int32_t i = 0; i < n; ++i) {
+    const int32_t some = std::min(num_layers - at, (int32_t)kCommitLayers);
+    for (int32_t i = 0; i < some; ++i) {
       const speechkv_layer_cache& y = layers[at + i];
       CommitLayer& c = a.layer[i];
       c.k_pages = y.cache.k_pages;
@@ -317,7 +342,7 @@ int speechkv_tree_commit(const speechkv_layer_cache* layers, int32_t num_layers,
       c.page_shift = log2_exact(y.cache.page_size);
       c.max_pages = y.cache.max_pages_per_seq;
     }
-    const hipError_t e = launch_commit(a, first.dtype, first.head_dim, n, batch, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_commit(a, first.dtype, first.head_dim, some, batch, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return SPEECHKV_ERR_HIP;
   }
   return SPEECHKV_OK;

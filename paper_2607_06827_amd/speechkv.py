@@ -329,6 +329,16 @@ def _int32(n) -> int:
     return n if -2**31 <= operator.index(n) < 2**31 else -1
 
 
+_INT32 = torch.int32
+
+
+def _int32_ptr(x: torch.Tensor, count: int, name: str) -> int:
+    """Address of one contiguous int32 value per sequence."""
+    if x.dtype != _INT32 or x.numel() != count or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor with one value per sequence")
+    return x.data_ptr()
+
+
 def _stream(stream) -> int:
     if stream is None:
         return _current_raw_stream(_current_device())
@@ -621,8 +631,8 @@ def speechkv_append_kv(k: torch.Tensor, v: torch.Tensor, cache: PagedKV, cache_l
     axis; q_out: [B, S, Hq, D] contiguous (or q itself); positions: int32
     [B, S]; inv_freq: fp32 [rotated elements / 2], or None: no rotation;
     cache_len, new_len, cache_len_out: int32 [B]."""
-    shape, strides, dt, int32 = k.shape, k.stride(), k.dtype, torch.int32
-    if shape != v.shape or strides != v.stride() or dt != v.dtype:
+    shape, strides, dt = k.shape, k.stride(), k.dtype
+    if v.shape != shape or v.stride() != strides or v.dtype != dt:
         raise ValueError("k and v must have one shape, one stride and one dtype")
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("k and v must be [B, S, Hkv, D] with a contiguous last axis")
@@ -642,26 +652,21 @@ def speechkv_append_kv(k: torch.Tensor, v: torch.Tensor, cache: PagedKV, cache_l
     c, pages, batch = cache._paged_kv_for(dt)
     if pages[1] != Hkv or pages[3] != D or batch != B:
         raise ValueError("k and v must have the cache's heads, head_dim and batch")
-    lens = []
-    for x in (cache_len, new_len, cache_len_out):
-        if x is None:
-            lens.append(None)
-        elif x.dtype != int32 or x.numel() != B or not x.is_contiguous():
-            raise ValueError("cache_len, new_len and cache_len_out must be contiguous int32 [B] tensors")
-        else:
-            lens.append(x.data_ptr())
+    lens = _int32_ptr(cache_len, B, "cache_len")
+    count = None if new_len is None else _int32_ptr(new_len, B, "new_len")
+    lens_out = None if cache_len_out is None else _int32_ptr(cache_len_out, B, "cache_len_out")
     rot, pos, inv = 0, None, None
     if inv_freq is not None:
         rot = 2 * inv_freq.numel()
         if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or rot > D:
             raise ValueError("inv_freq must be a contiguous fp32 tensor of at most head_dim / 2 entries")
-        if positions is None or positions.dtype != int32 or positions.shape != shape[:2] or \
+        if positions is None or positions.dtype != _INT32 or positions.shape != (B, S) or \
                 not positions.is_contiguous():
             raise ValueError("positions must be a contiguous int32 [B, S] tensor")
         pos, inv = positions.data_ptr(), inv_freq.data_ptr()
     st = _lib.speechkv_append_kv(qp, qs[0], qs[1], qs[2], Hq, k.data_ptr(), v.data_ptr(), strides[0],
-                                 strides[1], strides[2], B, S, lens[1], pos, inv, rot, _int32(rope), lens[0],
-                                 c, qop, lens[2], _stream(stream))
+                                 strides[1], strides[2], B, S, count, pos, inv, rot,
+                                 rope if rope == 0 or rope == 1 else -1, lens, c, qop, lens_out, _stream(stream))
     _check(st, "speechkv_append_kv")
 
 
@@ -680,18 +685,14 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
     c, pages, batch = cache._paged_kv_for(dt)
     if out.dtype != dt or pages[3] != D or batch != B:
         raise ValueError("q and out must have the cache's dtype, head_dim and batch")
-    if cache_len.dtype != torch.int32 or cache_len.numel() != B or not cache_len.is_contiguous():
-        raise ValueError("cache_len must be a contiguous int32 [B] tensor")
-    count, mask, mask_stride = None, None, 0
-    if num_nodes is not None:
-        if num_nodes.dtype != torch.int32 or num_nodes.numel() != B or not num_nodes.is_contiguous():
-            raise ValueError("num_nodes must be a contiguous int32 [B] tensor")
-        count = num_nodes.data_ptr()
+    lens = _int32_ptr(cache_len, B, "cache_len")
+    count = None if num_nodes is None else _int32_ptr(num_nodes, B, "num_nodes")
+    mask, mask_stride = None, 0
     if tree_mask is not None:
         mshape, words = tree_mask.shape, -(-n // 32)
         if len(mshape) == 3:
             mask_stride = n * words
-        if tree_mask.dtype != torch.int32 or not tree_mask.is_contiguous() or \
+        if tree_mask.dtype != _INT32 or not tree_mask.is_contiguous() or \
                 mshape != ((B, n, words) if mask_stride else (n, words)):
             raise ValueError("tree_mask must be contiguous int32 [B, n, ceil(n/32)] or [n, ceil(n/32)]")
         mask = tree_mask.data_ptr()
@@ -700,9 +701,9 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
     ws, ws_bytes = None, 0
     if workspace is not None:
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, c, cache_len.data_ptr(), _int32(max_cache_len),
-                                 count, mask, mask_stride, scale, _int32(num_splits), out.data_ptr(), ws,
-                                 ws_bytes, _stream(stream))
+    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, c, lens, _int32(max_cache_len),
+                                 count, mask, mask_stride, scale, num_splits and _int32(num_splits),
+                                 out.data_ptr(), ws, ws_bytes, _stream(stream))
     _check(st, "speechkv_tree_attn")
 
 
