@@ -136,12 +136,13 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s,
  *                value.
  * max_cache_len  host bound on cache_len (it sizes the grid); max_cache_len +
  *                num_nodes slots may exceed what a block table holds as long
- *                as the sequences' own slots do not.
+ *                as the sequences' own slots do not.  UNSUPPORTED from 2^31 -
+ *                8191 on.
  * scale          logit scale, finite and > 0.
  * num_splits     key ranges each (sequence, KV head) is split into; 0 selects
  *                speechkv_tree_num_splits().  Partial results are merged in a
  *                fixed order: the same call gives the same bits.  UNSUPPORTED
- *                where the launch would need 2^24 blocks or more.
+ *                where a launch would need 2^24 blocks or more.
  * workspace      device scratch of at least speechkv_tree_workspace_bytes(...)
  *                bytes (16-byte aligned; any contents); may be NULL when that
  *                size is 0.  Calls that overlap in time need one each.

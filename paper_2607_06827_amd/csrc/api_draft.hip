@@ -17,6 +17,10 @@ using namespace skv;
 // in 32 bits).
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
 
+// Longest cache of speechkv_tree_attn: the kernel's key numbers, with the nodes
+// and the 64 tiles that it looks ahead, stay in 31 bits.
+constexpr int32_t kMaxTreeLen = INT32_MAX - 8191;
+
 // Bytes from the first to past the last element of a strided [batch][rows]
 // [heads][dim] tensor, or -1 when they do not fit 2^62 (no tensor is so long).
 int64_t extent(int64_t batch, int64_t sb, int64_t rows, int64_t ss, int64_t heads, int64_t sh, int64_t dim,
@@ -234,7 +238,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   if ((int64_t)max_cache_len > (int64_t)cache->max_pages_per_seq * cache->page_size) return SPEECHKV_ERR_INVALID_ARG;
   if (num_q_heads < 1 || num_q_heads % cache->num_kv_heads) return SPEECHKV_ERR_INVALID_ARG;
   const int group = group_of(num_q_heads, cache->num_kv_heads);
-  if (group < 0) return SPEECHKV_ERR_UNSUPPORTED;
+  if (group < 0 || max_cache_len > kMaxTreeLen) return SPEECHKV_ERR_UNSUPPORTED;
   if (tree_mask && (mask_stride_b < 0 || mask_stride_b > ((int64_t)1 << 40))) return SPEECHKV_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned4(cache_len) || !aligned4(num_nodes_of) || !aligned4(tree_mask))
     return SPEECHKV_ERR_INVALID_ARG;
@@ -245,6 +249,8 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
   const int row_tiles = tree_row_tiles((int64_t)num_nodes * group, plan.groups);
   if (((int64_t)batch * cache->num_kv_heads * splits + 7) * row_tiles > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
+  if (splits > 1 && (int64_t)num_nodes * num_q_heads > kMaxBlocks * tree_merge_rows(cache->head_dim))
+    return SPEECHKV_ERR_UNSUPPORTED;
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;

@@ -101,6 +101,9 @@ constexpr int kTreeKeys = 32;  // keys of a tile
 // Blocks that the rows (nodes x heads of a group) of a (sequence, KV head) take,
 // of `groups` row groups of 32 each.
 inline int tree_row_tiles(int64_t rows, int groups) { return (int)((rows + 32 * groups - 1) / (32 * groups)); }
+// Rows (node, query head) of a sequence that a block of the merge takes.
+constexpr int kMergeThreads = 256;
+constexpr int tree_merge_rows(int head_dim) { return kMergeThreads / (head_dim / 4); }
 hipError_t launch_tree(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
 hipError_t launch_tree_merge(const TreeArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
 hipError_t launch_commit(const CommitArgs& a, int dtype, int head_dim, int layers, int batch, hipStream_t s);

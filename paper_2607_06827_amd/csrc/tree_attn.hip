@@ -707,11 +707,9 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
 
 // Log-sum-exp merge of the split partials of a (sequence, node, head) row, in
 // split order: D / 4 lanes a row, four elements a lane.
-constexpr int kMergeThreads = 256;
-
 template <typename T, int D>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs a) {
-  constexpr int kLanes = D / 4, kRows = kMergeThreads / kLanes;
+  constexpr int kLanes = D / 4, kRows = tree_merge_rows(D);
   const int b = blockIdx.y, e = threadIdx.x % kLanes;
   const int in = blockIdx.x * kRows + threadIdx.x / kLanes;  // (node, head) of the sequence
   const int n = a.nodes_of ? min(a.nodes_of[b], a.num_nodes) : a.num_nodes;
@@ -798,7 +796,7 @@ hipError_t launch_tree(const TreeArgs& a, int dtype, int head_dim, int batch, hi
 
 template <typename T, int D>
 hipError_t launch_merge_d(const TreeArgs& a, int batch, hipStream_t s) {
-  const int per = kMergeThreads / (D / 4);
+  const int per = tree_merge_rows(D);
   const dim3 grid((uint32_t)(((int64_t)a.num_nodes * a.num_q_heads + per - 1) / per), batch), block(kMergeThreads);
   return launch_struct(tree_merge_kernel<T, D>, grid, block, s, a);
 }

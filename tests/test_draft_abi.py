@@ -144,6 +144,22 @@ def test_tree_rejects_an_oversized_grid():
     assert tree(**dict(huge, splits=8000)) == E_HIP  # (2 x 1000 x 8000 blocks: the ranges do not meet)
 
 
+def test_tree_rejects_a_merge_the_device_cannot_count():
+    # 1024 x 480000 rows of 64 elements: 30 million blocks of 16 rows to merge, 8
+    # million of 128 rows to attend
+    wide = dict(c=cache(num_kv_heads=60000, num_pages=1), batch=1, n=1024, hq=480000, mask=None, ws=at(1 << 21), ws_bytes=1 << 40,
+                q=1 << 50, out=1 << 51, clen=1 << 52)
+    assert tree(splits=2, **wide) == E_UNS
+    assert tree(splits=1, **wide) != E_UNS
+
+
+def test_tree_rejects_caches_whose_keys_it_cannot_count():
+    c = cache(page_size=256, max_pages_per_seq=8388607)
+    far = dict(c=c, clen=1 << 50, q=1 << 51, out=1 << 52, mask=None)
+    assert tree(max_len=2**31 - 8191, **far) == E_UNS
+    assert tree(max_len=2**31 - 8192, **far) == E_HIP
+
+
 def test_tree_sizes():
     split, ws = skv.speechkv_tree_num_splits, skv.speechkv_tree_workspace_bytes
     BF, F32 = torch.bfloat16, torch.float32
