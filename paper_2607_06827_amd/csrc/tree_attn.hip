@@ -26,13 +26,21 @@
 // buffer, with no barrier: the next K tile is requested as soon as S^T is
 // computed, the next V tile as soon as O^T is, so a wave nearly always has a
 // tile in flight, and two blocks of 64 KB share a CU.  With two or four row
-// groups the waves of a stream load a tile together, one barrier per tile, one
-// (kGroups = 2) or three tiles ahead.
+// groups the waves of a stream load a tile together, one tile ahead, one barrier
+// per tile.  (Two tiles ahead are no faster, with or without a third block on a
+// CU.)
 //
-// Tiles below L need no mask.  In the others each lane has its row's 32 bits; a
-// row's weight of a key it does not see is 0, and since 0 times infinity is
-// not, a tile of these whose values are not all finite takes its products one
-// key at a time instead.
+// Tiles below L, or in a chain below the block's first node, need no mask (512
+// nodes behind 1000 keys: 53 -> 47 us).  In the others each lane has its row's 32
+// bits; a row's weight of a key it does not see is 0, and since 0 times infinity
+// is not, values of these tiles that are not finite become 0 and rows that do
+// see them get them after the loop, key by key.
+//
+// Measured (bf16, 128 wide): 16 sequences of 7692 keys, 32 nodes of 16 heads on
+// 8: 86 us, 508 MB at 5.9 TB/s (a copy reaches 5.1, reads alone 6.4); 64
+// sequences of up to 284 keys, 16 nodes: 16 us, 3.9 TB/s, 5 of them the launch
+// and a block's first loads; 8 sequences of up to 447 keys, 301 nodes of 64
+// heads on 8: 41 us, 590 TFLOP/s.
 //
 // Streams merge through LDS at the end, splits through the workspace, both by
 // log-sum-exp in a fixed order.
@@ -274,6 +282,11 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
   const int len_given = ((const_ptr)a.cache_len)[b];
   const int nodes_given = a.nodes_of ? ((const_ptr)a.nodes_of)[b] : n_alloc;
 
+  // Blocks behind a sequence's last node give up their place before they load
+  // anything (8 sequences of 109 to 301 nodes, 64 heads on 8: 47 -> 45 us); with
+  // one row tile there are none, and nothing waits for the count.
+  if (a.nodes_of && a.row_tiles > 1 && (row_tile * kRows) >> a.group_shift >= nodes_given) return;
+
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rg = wave % kGroups, stream = wave / kGroups;
   const int col = lane & 31, hg = lane >> 5;
@@ -431,8 +444,7 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = neg_inf(), l_run = 0.f;
 
-  // the 32 keys from kb on that this lane's row sees (a tile that reaches past
-  // len, or that lacks a page)
+  // the 32 keys from kb on that this lane's row sees
   auto tile_bits = [&](int kb, uint32_t present) __attribute__((always_inline)) -> uint32_t {
     uint32_t bits = ~0u;
     int lim = keys - kb;
@@ -501,8 +513,10 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1) + (kGroups ==
     }
   };
 
-  // A tile needs its bits where it reaches past len or lacks a page.
-  auto needs_bits = [&](int t, uint32_t present) { return t * kKeys + kKeys > len || present != ~0u; };
+  // A tile needs its bits where it reaches past the keys that every row of the
+  // block sees (in a chain those up to its first node's) or lacks a page.
+  const int seen = a.mask ? len : min(len + node0 + 1, keys);
+  auto needs_bits = [&](int t, uint32_t present) { return t * kKeys + kKeys > seen || present != ~0u; };
 
   if constexpr (kGroups == 1) {
     // every wave its own stream: K and V buffer of its own, no barrier
