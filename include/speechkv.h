@@ -29,6 +29,7 @@
  * instead of the one-run spans: speechkv_pool_kv_segments,
  * speechkv_prefill_attn_segments and their backward
  * speechkv_prefill_attn_bwd_segments and speechkv_pool_kv_bwd_segments.
+ * Steps of several new tokens over the cache are in speechkv_draft.h.
  *
  * Conventions shared by every call
  * --------------------------------

