@@ -248,6 +248,8 @@ SHAPES = [
     (F32, 64, 8, 2, 70, 10, 32, "tree", 1, 64),
     (F32, 128, 8, 2, 33, 30, 32, "chain", 1, 64),
     (F32, 64, 8, 8, 20, 20, 50, "dag", 3, 128),
+    (BF, 128, 16, 1, 3, 90, 1024, "tree", 1, 128),  # the longest mask rows, of one head each
+    (F32, 128, 8, 2, 2, 30, 1024, "tree", 1, 128),
 ]
 
 
