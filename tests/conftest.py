@@ -13,3 +13,28 @@ if HERE not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs an AMD GPU (gfx950) and the built HIP library")
+
+
+# Tests, by file, that make valid calls on made-up addresses: without a GPU they
+# end at the device (a HIP error), with one they would launch kernels there.
+VALID_CALLS_ON_FAKE_ADDRESSES = {
+    "test_draft_abi.py": (
+        "test_append_takes_queries_in_place_and_none_at_all",
+        "test_tree_valid_calls_reach_the_device",
+        "test_tree_rejects_an_oversized_grid",
+        "test_tree_rejects_a_merge_the_device_cannot_count",
+        "test_tree_rejects_caches_whose_keys_it_cannot_count",
+        "test_commit_valid_calls_reach_the_device",
+    ),
+}
+
+
+def pytest_collection_modifyitems(items):
+    import torch
+
+    if torch.cuda.device_count() == 0:
+        return
+    skip = pytest.mark.skip(reason="valid calls would launch kernels on the fake pointers")
+    for item in items:
+        if item.name in VALID_CALLS_ON_FAKE_ADDRESSES.get(item.path.name, ()):
+            item.add_marker(skip)
