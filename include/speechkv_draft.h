@@ -140,12 +140,17 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s,
  *                8191 on.
  * scale          logit scale, finite and > 0.
  * num_splits     key ranges each (sequence, KV head) is split into; 0 selects
- *                speechkv_tree_num_splits().  Partial results are merged in a
- *                fixed order: the same call gives the same bits.  UNSUPPORTED
- *                where a launch would need 2^24 blocks or more.
- * workspace      device scratch of at least speechkv_tree_workspace_bytes(...)
- *                bytes (16-byte aligned; any contents); may be NULL when that
- *                size is 0.  Calls that overlap in time need one each.
+ *                speechkv_tree_num_splits(), or the best count that the
+ *                workspace holds (1 needs none).  Partial results are merged in
+ *                a fixed order: the same call, with a workspace of the same
+ *                size, gives the same bits.  UNSUPPORTED where a launch would
+ *                need 2^24 blocks or more.
+ * workspace      device scratch (16-byte aligned; any contents), or NULL with
+ *                workspace_bytes not read.  With num_splits = 0 any size does;
+ *                a call that has less than speechkv_tree_workspace_bytes(...)
+ *                takes fewer splits, which may be slower.  With num_splits > 1
+ *                it must hold that size.  Calls that overlap in time need one
+ *                each.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP; ALIAS when out or the
  *         workspace overlaps q, the mask, the lengths, the block table, a page
  *         pool or each other.
@@ -158,9 +163,12 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes,
                        void* out, void* workspace, size_t workspace_bytes,
                        void* stream);
 
-/* The split count speechkv_tree_attn takes for num_splits = 0 (-1 for invalid
- * arguments), and the workspace it needs for num_splits (0: enough for its own
- * choice with either element type). */
+/* The split count speechkv_tree_attn takes for num_splits = 0 with workspace
+ * enough (-1 for invalid arguments), and the workspace it needs for num_splits
+ * (0: enough for its own choice with either element type).  The choice falls
+ * where more sequences, nodes or keys fill the chip without splits, so a larger
+ * call may need less: a program whose calls vary asks for every one of them, or
+ * keeps the largest size that it is ready to spend. */
 int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q_heads,
                                  int32_t num_kv_heads, int32_t head_dim, int32_t dtype,
                                  int32_t max_cache_len);

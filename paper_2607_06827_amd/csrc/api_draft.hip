@@ -70,7 +70,16 @@ struct TreePlan {
   int groups, splits;
 };
 
-// The plan with the smallest estimated time (the given split count, if any).
+// Bytes of the splits' partial rows: fp32 sums, then (running maximum, weight
+// sum) pairs.
+size_t tree_partial_bytes(int32_t batch, int32_t nodes, int32_t q_heads, int32_t head_dim, int32_t splits) {
+  return splits <= 1 ? 0 : (size_t)batch * nodes * q_heads * splits * (head_dim + 2) * sizeof(float);
+}
+
+// The plan with the smallest estimated time: of the given split count, or with
+// 0 of those whose partial rows fit `room` bytes.  (The best count falls where a
+// longer axis or more sequences fill the chip, so room for the largest call may
+// be too little for a smaller one's.)
 // The estimate is fitted to a sweep on MI355X over 24 shapes of 1 to 64
 // sequences, 1 to 8 KV heads, 4 to 1000 nodes and 30 to 7692 keys (bf16, 128
 // wide; the best of 1, 2 or 4 groups and of the split counts below is met
@@ -86,7 +95,8 @@ struct TreePlan {
 //  - splits cost 3.2 for the merge and the write and read of their fp32
 //    partial rows at 10 TB/s: one sequence of 7692 keys takes 71 us whole and
 //    16 in 16 splits, 64 sequences of 300 keys 19 us whole and 32 in two.
-TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, int dtype, int max_len, int splits) {
+TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, int dtype, int max_len, int splits,
+                   size_t room) {
   const bool f32 = dtype == SPEECHKV_DTYPE_F32, wide = head_dim == 128;
   const double rows = (double)nodes * group, units = (double)batch * kv_heads, size = head_dim / 128.0;
   const int64_t tiles = ((int64_t)max_len + nodes + kTreeKeys - 1) / kTreeKeys;
@@ -105,7 +115,7 @@ TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, 
     const double work_us = units * row_tiles * groups * tiles * busy_us / 1024;
     for (int i = 0; i < 10; ++i) {
       const int s = splits ? splits : counts[i];
-      if (!splits && s > tiles) break;
+      if (!splits && (s > tiles || tree_partial_bytes(batch, nodes, group * kv_heads, head_dim, s) > room)) break;
       const double steps = (double)(((tiles + s - 1) / s * groups + 3) / 4);
       const double full = units * row_tiles * s / slots;
       const double rounds = full >= 4 ? full + 0.5 : std::max(1.0, std::ceil(full));
@@ -119,12 +129,6 @@ TreePlan tree_plan(int batch, int nodes, int group, int kv_heads, int head_dim, 
     }
   }
   return best;
-}
-
-// Bytes of the splits' partial rows: fp32 sums, then (running maximum, weight
-// sum) pairs.
-size_t tree_partial_bytes(int32_t batch, int32_t nodes, int32_t q_heads, int32_t head_dim, int32_t splits) {
-  return splits <= 1 ? 0 : (size_t)batch * nodes * q_heads * splits * (head_dim + 2) * sizeof(float);
 }
 
 }  // namespace
@@ -210,7 +214,7 @@ int32_t speechkv_tree_num_splits(int32_t batch, int32_t num_nodes, int32_t num_q
     return -1;
   const int group = group_of(num_q_heads, num_kv_heads);
   if (group < 0) return -1;
-  return tree_plan(batch, num_nodes, group, num_kv_heads, head_dim, dtype, max_cache_len, 0).splits;
+  return tree_plan(batch, num_nodes, group, num_kv_heads, head_dim, dtype, max_cache_len, 0, SIZE_MAX).splits;
 }
 
 size_t speechkv_tree_workspace_bytes(int32_t batch, int32_t num_nodes, int32_t num_q_heads, int32_t num_kv_heads,
@@ -243,7 +247,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   if (!aligned16(q) || !aligned16(out) || !aligned4(cache_len) || !aligned4(num_nodes_of) || !aligned4(tree_mask))
     return SPEECHKV_ERR_INVALID_ARG;
   const TreePlan plan = tree_plan(batch, num_nodes, group, cache->num_kv_heads, cache->head_dim, cache->dtype,
-                                  max_cache_len, num_splits);
+                                  max_cache_len, num_splits, workspace ? workspace_bytes : 0);
   const int32_t splits = plan.splits;
   const size_t need = tree_partial_bytes(batch, num_nodes, num_q_heads, cache->head_dim, splits);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;

@@ -677,7 +677,8 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
                        stream=None) -> None:
     """q, out: [B, n, Hq, D] contiguous; tree_mask: int32 words of bits
     [B, n, ceil(n/32)], or [n, ceil(n/32)] for every sequence alike (see
-    tree_mask()), or None: a chain; cache_len, num_nodes: int32 [B]."""
+    tree_mask()), or None: a chain; cache_len, num_nodes: int32 [B]; workspace:
+    device bytes, of any size with num_splits = 0 (too few: fewer splits)."""
     shape, dt = q.shape, q.dtype
     if len(shape) != 4 or out.shape != shape or not q.is_contiguous() or not out.is_contiguous():
         raise ValueError("q and out must be contiguous [B, n, Hq, D] tensors of one shape")
