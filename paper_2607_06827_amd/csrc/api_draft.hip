@@ -17,6 +17,10 @@ using namespace skv;
 // in 32 bits).
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
 
+// The kernels hold a mask row's words and a path's entries in LDS arrays.
+static_assert(32 * kMaskWords >= SPEECHKV_MAX_TREE_NODES && kCommitPath >= SPEECHKV_MAX_TREE_NODES,
+              "arrays of a tree's nodes");
+
 // Longest cache of speechkv_tree_attn: the kernel's key numbers, with the nodes
 // and the 64 tiles that it looks ahead, stay in 31 bits.
 constexpr int32_t kMaxTreeLen = INT32_MAX - 8191;

@@ -54,9 +54,9 @@ namespace {
 // The running maximum may lag the true one by up to 2^kSlack before the sums are
 // rescaled; the division by the weight sum makes the choice exact.
 constexpr float kSlack = 8.f;
-constexpr int kKeys = 32;   // keys per tile
+constexpr int kKeys = kTreeKeys;  // keys per tile
+static_assert(kKeys == 32, "a tile's keys are the bits of a word and the rows of a 32x32 product");
 constexpr int kWaves = 4;
-constexpr int kMaskWords = 32;  // most words of a mask row (SPEECHKV_MAX_TREE_NODES / 32)
 constexpr int kSpreadUnits = 32;  // units from which an XCD keeps a unit's row tiles together
 
 // Layout of a K or V tile in LDS: rows of kChunks 16-byte chunks, chunk c of
