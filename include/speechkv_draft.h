@@ -137,7 +137,7 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s,
  * max_cache_len  host bound on cache_len (it sizes the grid); max_cache_len +
  *                num_nodes slots may exceed what a block table holds as long
  *                as the sequences' own slots do not.  UNSUPPORTED from 2^31 -
- *                8191 on.
+ *                8191 on, and with thousands of splits from up to 2^21 less.
  * scale          logit scale, finite and > 0.
  * num_splits     key ranges each (sequence, KV head) is split into; 0 selects
  *                speechkv_tree_num_splits(), or the best count that the

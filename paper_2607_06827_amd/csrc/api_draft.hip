@@ -22,7 +22,8 @@ static_assert(32 * kMaskWords >= SPEECHKV_MAX_TREE_NODES && kCommitPath >= SPEEC
               "arrays of a tree's nodes");
 
 // Longest cache of speechkv_tree_attn: the kernel's key numbers, with the nodes
-// and the 64 tiles that it looks ahead, stay in 31 bits.
+// and the tiles that it looks ahead, stay in 31 bits.  (Splits are whole tiles,
+// so many of them reach further; those calls are checked by their own numbers.)
 constexpr int32_t kMaxTreeLen = INT32_MAX - 8191;
 
 // Bytes from the first to past the last element of a strided [batch][rows]
@@ -259,6 +260,9 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   if (((int64_t)batch * cache->num_kv_heads * splits + 7) * row_tiles > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
   if (splits > 1 && (int64_t)num_nodes * num_q_heads > kMaxBlocks * tree_merge_rows(cache->head_dim))
     return SPEECHKV_ERR_UNSUPPORTED;
+  const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;
+  const int64_t tiles_per_split = (tiles + splits - 1) / splits;
+  if ((tiles_per_split * splits + kTreeAhead) * kTreeKeys > (int64_t)INT32_MAX + 1) return SPEECHKV_ERR_UNSUPPORTED;
   const int words = (num_nodes + 31) / 32;
   const int64_t qo = (int64_t)batch * num_nodes * num_q_heads * cache->head_dim * elt_size(cache->dtype);
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4;
@@ -286,8 +290,7 @@ int speechkv_tree_attn(const void* q, int32_t batch, int32_t num_nodes, int32_t 
   a.row_tiles = row_tiles;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.num_splits = splits;
-  const int64_t tiles = ((int64_t)max_cache_len + num_nodes + kTreeKeys - 1) / kTreeKeys;
-  a.tiles_per_split = (int)((tiles + splits - 1) / splits);
+  a.tiles_per_split = (int)tiles_per_split;
   a.out = out;
   a.ws_o = nullptr;
   a.ws_ml = nullptr;

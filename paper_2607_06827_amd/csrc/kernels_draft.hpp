@@ -99,6 +99,7 @@ static_assert(sizeof(CommitArgs) <= 4096, "kernel arguments");
 // dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, int batch, hipStream_t s);
 constexpr int kTreeKeys = 32;  // keys of a tile
+constexpr int kTreeAhead = 64;  // tiles that a block looks ahead: 16 steps of four streams
 constexpr int kMaskWords = 32;  // most words of a mask row (SPEECHKV_MAX_TREE_NODES / 32)
 // Blocks that the rows (nodes x heads of a group) of a (sequence, KV head) take,
 // of `groups` row groups of 32 each.
