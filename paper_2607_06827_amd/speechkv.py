@@ -665,8 +665,9 @@ def speechkv_append_kv(k: torch.Tensor, v: torch.Tensor, cache: PagedKV, cache_l
             raise ValueError("positions must be a contiguous int32 [B, S] tensor")
         pos, inv = positions.data_ptr(), inv_freq.data_ptr()
     st = _lib.speechkv_append_kv(qp, qs[0], qs[1], qs[2], Hq, k.data_ptr(), v.data_ptr(), strides[0],
-                                 strides[1], strides[2], B, S, count, pos, inv, rot,
-                                 rope if rope == 0 or rope == 1 else -1, lens, c, qop, lens_out, _stream(stream))
+                                 strides[1], strides[2], B if B < 2**31 else -1, S if S < 2**31 else -1,
+                                 count, pos, inv, rot, rope if rope == 0 or rope == 1 else -1, lens, c, qop,
+                                 lens_out, _stream(stream))
     _check(st, "speechkv_append_kv")
 
 
@@ -702,9 +703,9 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
     ws, ws_bytes = None, 0
     if workspace is not None:
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = _lib.speechkv_tree_attn(q.data_ptr(), B, n, Hq, c, lens, _int32(max_cache_len),
-                                 count, mask, mask_stride, scale, num_splits and _int32(num_splits),
-                                 out.data_ptr(), ws, ws_bytes, _stream(stream))
+    st = _lib.speechkv_tree_attn(q.data_ptr(), B if B < 2**31 else -1, n, Hq, c, lens,
+                                 _int32(max_cache_len), count, mask, mask_stride, scale,
+                                 num_splits and _int32(num_splits), out.data_ptr(), ws, ws_bytes, _stream(stream))
     _check(st, "speechkv_tree_attn")
 
 
@@ -730,8 +731,8 @@ def speechkv_tree_commit(layers: CacheStack, path: torch.Tensor, path_len: torch
             path_len.dtype != torch.int32 or not path_len.is_contiguous() or \
             path.shape[0] != layers.batch or path_len.numel() != layers.batch:
         raise ValueError("path and path_len must be contiguous int32 [B, max_path] and [B] tensors")
-    st = _lib.speechkv_tree_commit(layers._packed, layers.num_layers, layers.batch, path.data_ptr(),
-                                   path.shape[1], path_len.data_ptr(), _int32(num_nodes), _stream(stream))
+    st = _lib.speechkv_tree_commit(layers._packed, layers.num_layers, _int32(layers.batch), path.data_ptr(),
+                                   _int32(path.shape[1]), path_len.data_ptr(), _int32(num_nodes), _stream(stream))
     _check(st, "speechkv_tree_commit")
 
 
