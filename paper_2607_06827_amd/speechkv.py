@@ -702,6 +702,8 @@ def speechkv_tree_attn(q: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
         scale = D ** -0.5
     ws, ws_bytes = None, 0
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     st = _lib.speechkv_tree_attn(q.data_ptr(), B if B < 2**31 else -1, n, Hq, c, lens,
                                  _int32(max_cache_len), count, mask, mask_stride, scale,

@@ -1,6 +1,6 @@
 """What the binding of the steps of several new tokens hands to the library:
-counts that int32 does not hold are its invalid argument, not their low bits
-(CPU, no kernel is launched)."""
+counts that int32 does not hold are its invalid argument, not their low bits,
+and a workspace is one piece of memory (CPU, no kernel is launched)."""
 import pytest
 import torch
 
@@ -78,3 +78,12 @@ def test_commit_refuses_more_sequences_than_int32_holds(monkeypatch):
     got = stub(monkeypatch, "speechkv_tree_commit")
     skv.speechkv_tree_commit(stack, path, path[:, 0], 5, stream=0)
     assert got[0][2] == -1
+
+
+@pytest.mark.parametrize("ws", [torch.empty(1, dtype=torch.uint8).expand(1 << 20),
+                                torch.empty(1 << 12, dtype=torch.float32)[::2],
+                                torch.empty(64, 64).t()])
+def test_tree_refuses_a_workspace_that_is_not_one_piece(ws):
+    x = host()
+    with pytest.raises(ValueError):
+        skv.speechkv_tree_attn(x["q"], x["cache"], x["lens"], 5, x["q"].clone(), workspace=ws, stream=0)
