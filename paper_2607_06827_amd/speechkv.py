@@ -216,10 +216,11 @@ class PagedKV(_Description):
         pages, heads, page, dim = shape
         try:
             return _pack_paged_kv(k.data_ptr(), v.data_ptr(), t.data_ptr(), pages, page, table[1],
-                                  heads, dim, _dtype_code(dtype)), shape, table[0]
+                                  heads, dim, _DTYPE_CODES.get(dtype, 99)), shape, table[0]
         except struct.error:
             return _pack_paged_kv(k.data_ptr(), v.data_ptr(), t.data_ptr(),
-                                  *_int32s(pages, page, table[1], heads, dim), _dtype_code(dtype)), shape, table[0]
+                                  *_int32s(pages, page, table[1], heads, dim),
+                                  _DTYPE_CODES.get(dtype, 99)), shape, table[0]
 
 
 @dataclasses.dataclass
@@ -312,12 +313,11 @@ class CacheStack:
         self._packed = b"".join(packed)
 
 
+_DTYPE_CODES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
 def _dtype_code(dt: torch.dtype) -> int:
-    if dt == torch.bfloat16:
-        return DTYPE_BF16
-    if dt == torch.float32:
-        return DTYPE_F32
-    return 99  # the library rejects it as unsupported
+    return _DTYPE_CODES.get(dt, 99)  # the library rejects others as unsupported
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -729,12 +729,15 @@ def speechkv_tree_commit(layers: CacheStack, path: torch.Tensor, path_len: torch
     sequence of the tree."""
     if not isinstance(layers, CacheStack):
         raise TypeError(f"{type(layers).__name__} given where the call takes a CacheStack")
-    if path.dtype != torch.int32 or path.dim() != 2 or not path.is_contiguous() or \
-            path_len.dtype != torch.int32 or not path_len.is_contiguous() or \
-            path.shape[0] != layers.batch or path_len.numel() != layers.batch:
+    B, shape = layers.batch, path.shape
+    if path.dtype != _INT32 or len(shape) != 2 or not path.is_contiguous() or \
+            path_len.dtype != _INT32 or not path_len.is_contiguous() or \
+            shape[0] != B or path_len.numel() != B:
         raise ValueError("path and path_len must be contiguous int32 [B, max_path] and [B] tensors")
-    st = _lib.speechkv_tree_commit(layers._packed, layers.num_layers, _int32(layers.batch), path.data_ptr(),
-                                   _int32(path.shape[1]), path_len.data_ptr(), _int32(num_nodes), _stream(stream))
+    most = shape[1]
+    st = _lib.speechkv_tree_commit(layers._packed, layers.num_layers, B if B < 2**31 else -1, path.data_ptr(),
+                                   most if most < 2**31 else -1, path_len.data_ptr(), _int32(num_nodes),
+                                   _stream(stream))
     _check(st, "speechkv_tree_commit")
 
 
