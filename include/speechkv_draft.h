@@ -114,7 +114,10 @@ int speechkv_append_kv(const void* q, int64_t q_stride_b, int64_t q_stride_s,
  *   out[b][i][h] = sum_c softmax_c(scale * q[b][i][h] . K[b, c, g]) V[b, c, g]
  * over what it sees, and 0 if it sees nothing (L = 0 and an empty mask row).
  * What a node does not see does not reach its output, whatever it holds
- * (infinities and NaN included).
+ * (infinities and NaN included).  With bf16 the softmax weights are rounded to
+ * bf16 (by 2^-8 of each at most) before their products with V, as in
+ * speechkv_decode_attn; maxima, sums and the outputs before their rounding are
+ * fp32, and so is everything with fp32.
  *
  * q, out         device, element type cache->dtype,
  *                [batch][num_nodes][num_q_heads][head_dim], dense.  Rows

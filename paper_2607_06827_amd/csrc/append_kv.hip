@@ -10,7 +10,7 @@
 // A block moves one token, a thread two 8-element chunks of a head: the two
 // whose elements turn together, or two of the elements that stay.  Each angle's
 // sine and cosine are computed once, by a thread of their own, and shared
-// through LDS (1024 tokens of 16 + 16 heads 7.1 -> 5.5 us).  Several tokens a
+// through LDS (1024 tokens of 16 + 16 heads 7.1 -> 5.3 us).  Several tokens a
 // block, or rows requested before the angles, are no faster.  Bound by HBM:
 // 12768 tokens of 16 + 16 heads take 40 us, 209 MB at 5.2 TB/s; a large copy
 // reaches 5.1.

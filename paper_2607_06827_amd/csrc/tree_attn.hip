@@ -15,8 +15,16 @@
 //     S^T = K Q^T      (keys x rows; 32x32 MFMA, A = K tile, B = Q^T)
 //     O^T += V^T P^T   (A = V^T tile, B = P^T, straight from S^T's layout)
 // with the online softmax between them, one row per lane column.  bf16 takes
-// v_mfma_f32_32x32x16_bf16 with the weights rounded to bf16 and fp32 sums,
-// fp32 takes v_mfma_f32_32x32x2_f32.
+// v_mfma_f32_32x32x16_bf16, fp32 takes v_mfma_f32_32x32x2_f32; maxima, weight
+// sums and outputs are fp32 in both.
+//
+// The bf16 product wants the weights in bf16, so they are rounded, as this
+// library's decode and prefill do; the weight sum is of those before, so an
+// output is off by at most 2^-8 of its weighted |values| and its own rounding.
+// Measured against 64 bits: 2.1 to 2.3e-3 (root mean square, relative), 1.7e-3
+// of it the output's rounding.  Weights as the sum of two bf16 numbers leave that
+// alone, but take the value products twice: 16 sequences of 7692 keys 91 -> 93
+// us, one with 64 nodes 17.8 -> 19.8, 301 nodes of 64 heads on 8 43 -> 52.
 //
 // K/V tiles go from the paged cache straight into LDS (direct loads of 16 bytes
 // a lane), rows unpadded and their 16-byte chunks XOR-swizzled so that operand

@@ -9,9 +9,10 @@
 // for all heads: the block looks it up once, an entry a thread, into LDS.
 //
 // Bound by the chain of loads (length, path, table entries, rows) where little
-// moves (one layer of one user: 2.9 us) and by HBM where much does (paths of up
-// to 6 of 64 users through 28 layers of 8 KV heads: 10 us, 36 MB at 3.5 TB/s; 38
-// us with a block for each KV head and pool).
+// moves (one layer of one user: 2.9 us).  Paths of up to 6 of 64 users through
+// 28 layers of 8 KV heads take 10 us, 38 with a block for each KV head and pool;
+// with a third of the entries moving (the others stay where they are) that is
+// 15 MB read and written, 1.5 TB/s, so not HBM's rate.
 #include <algorithm>
 
 #include "kernels_draft.hpp"
