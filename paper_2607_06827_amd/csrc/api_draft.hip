@@ -13,10 +13,6 @@ namespace {
 
 using namespace skv;
 
-// Most blocks of 256 threads along one axis of a launch (its threads are counted
-// in 32 bits).
-constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
-
 // The kernels hold a mask row's words and a path's entries in LDS arrays.
 static_assert(32 * kMaskWords >= SPEECHKV_MAX_TREE_NODES && kCommitPath >= SPEECHKV_MAX_TREE_NODES,
               "arrays of a tree's nodes");
@@ -25,18 +21,6 @@ static_assert(32 * kMaskWords >= SPEECHKV_MAX_TREE_NODES && kCommitPath >= SPEEC
 // and the tiles that it looks ahead, stay in 31 bits.  (Splits are whole tiles,
 // so many of them reach further; those calls are checked by their own numbers.)
 constexpr int32_t kMaxTreeLen = INT32_MAX - 8191;
-
-// Bytes from the first to past the last element of a strided [batch][rows]
-// [heads][dim] tensor, or -1 when they do not fit 2^62 (no tensor is so long).
-int64_t extent(int64_t batch, int64_t sb, int64_t rows, int64_t ss, int64_t heads, int64_t sh, int64_t dim,
-               int64_t elt) {
-  const __int128 n = ((__int128)(batch - 1) * sb + (__int128)(rows - 1) * ss + (__int128)(heads - 1) * sh + dim) * elt;
-  return n < ((__int128)1 << 62) ? (int64_t)n : -1;
-}
-
-bool bad_stride(int64_t s, int64_t per16) { return s < 0 || s % per16; }
-
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Whether a region of one list overlaps a region of another (null ones take no
 // part).  Lists that lie apart as a whole, as pools and lengths mostly do, are
@@ -66,8 +50,6 @@ bool meet(int na, const A& a, int nb, const B& b) {
   }
   return false;
 }
-
-int64_t table_bytes(const speechkv_paged_kv* c, int32_t batch) { return (int64_t)batch * c->max_pages_per_seq * 4; }
 
 // How speechkv_tree_attn cuts a call: row groups of a block (1, 2 or 4, of 32
 // rows each) and splits of the keys.

@@ -14,6 +14,10 @@ namespace skv {
 constexpr int kMaxGrid = 65535;
 constexpr int kMaxRows = 2147483647 - SPEECHKV_MAX_WINDOW;  // ceil(T / w) stays in int32
 
+// Most blocks of 256 threads along one axis of a launch (its threads are counted
+// in 32 bits).
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline int elt_size(int dtype) { return dtype == SPEECHKV_DTYPE_BF16 ? 2 : 4; }
@@ -57,6 +61,20 @@ inline int group_of(int num_q_heads, int num_kv_heads) {
 inline int64_t page_pool_bytes(const speechkv_paged_kv* c) {
   return (int64_t)c->num_pages * c->num_kv_heads * c->page_size * c->head_dim * elt_size(c->dtype);
 }
+
+inline int64_t table_bytes(const speechkv_paged_kv* c, int32_t batch) { return (int64_t)batch * c->max_pages_per_seq * 4; }
+
+// Bytes from the first to past the last element of a strided [batch][rows]
+// [heads][dim] tensor, or -1 when they do not fit 2^62 (no tensor is so long).
+inline int64_t extent(int64_t batch, int64_t sb, int64_t rows, int64_t ss, int64_t heads, int64_t sh, int64_t dim,
+               int64_t elt) {
+  const __int128 n = ((__int128)(batch - 1) * sb + (__int128)(rows - 1) * ss + (__int128)(heads - 1) * sh + dim) * elt;
+  return n < ((__int128)1 << 62) ? (int64_t)n : -1;
+}
+
+inline bool bad_stride(int64_t s, int64_t per16) { return s < 0 || s % per16; }
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 inline bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);

@@ -1,5 +1,5 @@
-"""ctypes binding of libspeechkv.so (include/speechkv.h and
-include/speechkv_draft.h), same names as the C ABI.
+"""ctypes binding of libspeechkv.so (include/speechkv.h, speechkv_draft.h and
+speechkv_norm.h), same names as the C ABI.
 
 Argument marshalling only: tensors become device pointers, strides and sizes
 become integers, and a non-zero status becomes a SpeechKVError.  Every step of
@@ -71,6 +71,20 @@ class _LayerCache(ctypes.Structure):
     _fields_ = [("cache", _PagedKV), ("cache_len", ctypes.c_void_p), ("cache_len_out", ctypes.c_void_p)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_s", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("num_heads", ctypes.c_int32)]
+
+
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("num_axes", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
 # The descriptions above as packed bytes, passed by address: filling a cache
 # description takes 1.0 us instead of 1.7 with a ctypes structure, and a
 # decoding step of one sequence is bound by this path.  ctypes then takes any
@@ -80,6 +94,9 @@ _pack_paged_kv = struct.Struct("@PPPiiiiii").pack
 _pack_spans = struct.Struct("@PPPii").pack
 _pack_segments = struct.Struct("@PPPiii4x").pack  # (padded to the structure's 8-byte alignment)
 _pack_lens = struct.Struct("@PP").pack  # what follows the cache in a layer of a CacheStack
+_pack_heads = struct.Struct("@Pqqqi4x").pack
+_pack_norm = struct.Struct("@PPf4x").pack
+_pack_rope = struct.Struct("@PPPiii4x").pack
 
 
 def _int32s(*counts):
@@ -153,6 +170,15 @@ _lib.speechkv_tree_num_splits.argtypes = [_i32] * 7
 _lib.speechkv_tree_num_splits.restype = _i32
 _lib.speechkv_tree_workspace_bytes.argtypes = [_i32] * 7
 _lib.speechkv_tree_workspace_bytes.restype = _sz
+_lib.speechkv_norm_rope.argtypes = [_vp, _vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.speechkv_norm_rope.restype = ctypes.c_int
+_lib.speechkv_norm_rope_bwd.argtypes = [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                        _vp, _vp, _sz, _vp]
+_lib.speechkv_norm_rope_bwd.restype = ctypes.c_int
+_lib.speechkv_norm_rope_bwd_workspace_bytes.argtypes = [_i32] * 5
+_lib.speechkv_norm_rope_bwd_workspace_bytes.restype = _sz
+_lib.speechkv_norm_append_kv.argtypes = [_vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.speechkv_norm_append_kv.restype = ctypes.c_int
 _lib.speechkv_compressed_len.argtypes = [_i32] * 6
 _lib.speechkv_compressed_len.restype = _i64
 _lib.speechkv_decode_num_splits.argtypes = [_i32, _i32, _i32]
@@ -284,6 +310,29 @@ class Segments(_Description):
                         max([sum(t + s for t, s in x) for x in segs] or [0]))
 
 
+class Rope:
+    """The rotation of speechkv_norm_rope and its kin: positions int32 [B, S],
+    or [axes, B, S] with axis int32 [rotated elements / 2] naming each pair's
+    axis (None: the first); inv_freq fp32 [rotated elements / 2]; layout
+    ROPE_HALVES or ROPE_PAIRS.  It keeps its tensors alive."""
+
+    def __init__(self, positions, inv_freq, axis=None, layout=ROPE_HALVES):
+        if positions.dtype != torch.int32 or positions.dim() not in (2, 3) or not positions.is_contiguous():
+            raise ValueError("positions must be a contiguous int32 [B, S] or [axes, B, S] tensor")
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous fp32 tensor of one axis")
+        if axis is not None and (axis.dtype != torch.int32 or axis.shape != inv_freq.shape or
+                                 not axis.is_contiguous()):
+            raise ValueError("axis must be a contiguous int32 tensor of inv_freq's shape")
+        if layout not in (ROPE_HALVES, ROPE_PAIRS):
+            raise ValueError("layout must be ROPE_HALVES or ROPE_PAIRS")
+        self.rows = tuple(positions.shape[-2:])
+        self._keep = (positions, inv_freq, axis)
+        axes = positions.shape[0] if positions.dim() == 3 else 1
+        self._packed = _pack_rope(positions.data_ptr(), inv_freq.data_ptr(), 0 if axis is None else axis.data_ptr(),
+                                  *_int32s(axes, 2 * inv_freq.numel(), layout))
+
+
 class CacheStack:
     """The caches of a model's layers with their lengths, for
     speechkv_tree_commit: caches is a list of PagedKV, cache_lens and
@@ -337,6 +386,15 @@ def _int32_ptr(x: torch.Tensor, count: int, name: str) -> int:
     if x.dtype != _INT32 or x.numel() != count or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor with one value per sequence")
     return x.data_ptr()
+
+
+def _workspace(x: Optional[torch.Tensor]):
+    """Address and bytes of a workspace, (None, 0) without one."""
+    if x is None:
+        return None, 0
+    if not x.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return x.data_ptr(), x.numel() * x.element_size()
 
 
 def _stream(stream) -> int:
@@ -761,6 +819,112 @@ def tree_mask(parents, device="cuda") -> torch.Tensor:
         rows.append([[(s >> 32 * w & 0xffffffff) - (s >> 32 * w & 0x80000000) * 2 for w in range(words)]
                      for s in see])
     return torch.tensor(rows, dtype=torch.int32, device=device)
+
+
+def _heads(x: Optional[torch.Tensor], rows, dtype) -> Optional[bytes]:
+    """The packed description of rows [B, S, H, D]; rows is (B, S, D)."""
+    if x is None:
+        return None
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 4 or strides[3] != 1:
+        raise ValueError("queries, keys and values must be [B, S, H, D] with a contiguous last axis")
+    if (shape[0], shape[1], shape[3]) != rows or x.dtype != dtype:
+        raise ValueError("queries, keys and values must share batch, rows, head_dim and dtype")
+    return _pack_heads(x.data_ptr(), strides[0], strides[1], strides[2], _int32(shape[2]))
+
+
+def _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise):
+    """(packed norm, packed rotation, address of the row counts) of a call."""
+    for g in (gamma_q, gamma_k):
+        if g is not None and (g.dtype != torch.float32 or g.numel() != rows[2] or not g.is_contiguous() or
+                              not normalise):
+            raise ValueError("gamma_q and gamma_k are contiguous fp32 [head_dim] tensors, of a norm")
+    norm = _pack_norm(0 if gamma_q is None else gamma_q.data_ptr(), 0 if gamma_k is None else gamma_k.data_ptr(),
+                      eps) if normalise else None
+    if rope is not None:
+        if not isinstance(rope, Rope):
+            raise TypeError(f"{type(rope).__name__} given where the call takes a Rope")
+        if rope.rows != rows[:2]:
+            raise ValueError("the rotation's positions must be of the call's batch and rows")
+        rope = rope._packed
+    return norm, rope, None if row_len is None else _int32_ptr(row_len, rows[0], "row_len")
+
+
+def speechkv_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+                       k_out: Optional[torch.Tensor], gamma_q: Optional[torch.Tensor] = None,
+                       gamma_k: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[Rope] = None,
+                       row_len: Optional[torch.Tensor] = None, normalise: bool = True, stream=None) -> None:
+    """q, q_out: [B, S, Hq, D] and k, k_out: [B, S, Hkv, D] views with a
+    contiguous last axis (q and q_out, or k and k_out, may be None; an output
+    may be its input); gamma_q, gamma_k: fp32 [D] or None: 1; row_len: int32
+    [B] or None: every row; normalise=False: the rotation alone."""
+    x = k if q is None else q
+    if x is None or len(x.shape) != 4:
+        raise ValueError("q or k must be given, as [B, S, H, D]")
+    B, S, _, D = x.shape
+    rows, dt = (B, S, D), x.dtype
+    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
+    st = _lib.speechkv_norm_rope(_heads(q, rows, dt), _heads(k, rows, dt), _int32(B), _int32(S), count, _int32(D),
+                                 _dtype_code(dt), norm, turn, _heads(q_out, rows, dt), _heads(k_out, rows, dt),
+                                 _stream(stream))
+    _check(st, "speechkv_norm_rope")
+
+
+def speechkv_norm_rope_bwd_workspace_bytes(batch: int, num_rows: int, num_q_heads: int, num_kv_heads: int,
+                                           head_dim: int) -> int:
+    return int(_lib.speechkv_norm_rope_bwd_workspace_bytes(batch, num_rows, num_q_heads, num_kv_heads, head_dim))
+
+
+def speechkv_norm_rope_bwd(q: Optional[torch.Tensor], k: Optional[torch.Tensor], dq_out: Optional[torch.Tensor],
+                           dk_out: Optional[torch.Tensor], dq: Optional[torch.Tensor], dk: Optional[torch.Tensor],
+                           gamma_q: Optional[torch.Tensor] = None, gamma_k: Optional[torch.Tensor] = None,
+                           eps: float = 1e-6, rope: Optional[Rope] = None, row_len: Optional[torch.Tensor] = None,
+                           dgamma_q: Optional[torch.Tensor] = None, dgamma_k: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, normalise: bool = True, stream=None) -> None:
+    """q, k: the forward's inputs; dq_out, dk_out: gradients of its outputs; dq,
+    dk: gradients of its inputs (dq may be dq_out, dk may be dk_out); dgamma_q,
+    dgamma_k: fp32 [D] or None; workspace: device bytes, with a dgamma.  The
+    rest as for speechkv_norm_rope."""
+    x = k if q is None else q
+    if x is None or len(x.shape) != 4:
+        raise ValueError("q or k must be given, as [B, S, H, D]")
+    B, S, _, D = x.shape
+    rows, dt = (B, S, D), x.dtype
+    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
+    for g in (dgamma_q, dgamma_k):
+        if g is not None and (g.dtype != torch.float32 or g.numel() != D or not g.is_contiguous()):
+            raise ValueError("dgamma_q and dgamma_k are contiguous fp32 [head_dim] tensors")
+    ws, ws_bytes = _workspace(workspace)
+    st = _lib.speechkv_norm_rope_bwd(_heads(q, rows, dt), _heads(k, rows, dt), _heads(dq_out, rows, dt),
+                                     _heads(dk_out, rows, dt), _int32(B), _int32(S), count, _int32(D),
+                                     _dtype_code(dt), norm, turn, _heads(dq, rows, dt), _heads(dk, rows, dt),
+                                     _ptr(dgamma_q), _ptr(dgamma_k), ws, ws_bytes, _stream(stream))
+    _check(st, "speechkv_norm_rope_bwd")
+
+
+def speechkv_norm_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: PagedKV,
+                            cache_len: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                            gamma_q: Optional[torch.Tensor] = None, gamma_k: Optional[torch.Tensor] = None,
+                            eps: float = 1e-6, rope: Optional[Rope] = None, new_len: Optional[torch.Tensor] = None,
+                            cache_len_out: Optional[torch.Tensor] = None, normalise: bool = True,
+                            stream=None) -> None:
+    """k, v: [B, S, Hkv, D] and q, q_out: [B, S, Hq, D] views with a contiguous
+    last axis (q and q_out may be None, q_out may be q); cache_len, new_len,
+    cache_len_out: int32 [B].  The rest as for speechkv_norm_rope."""
+    if len(k.shape) != 4:
+        raise ValueError("k must be [B, S, Hkv, D]")
+    B, S, _, D = k.shape
+    rows, dt = (B, S, D), k.dtype
+    c, pages, batch = cache._paged_kv_for(dt)
+    if pages[3] != D or batch != B:
+        raise ValueError("k and v must have the cache's head_dim and batch")
+    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, new_len, normalise)
+    lens = _int32_ptr(cache_len, B, "cache_len")
+    lens_out = None if cache_len_out is None else _int32_ptr(cache_len_out, B, "cache_len_out")
+    st = _lib.speechkv_norm_append_kv(_heads(q, rows, dt), _heads(k, rows, dt), _heads(v, rows, dt), _int32(B),
+                                      _int32(S), count, norm, turn, lens, c, _heads(q_out, rows, dt), lens_out,
+                                      _stream(stream))
+    _check(st, "speechkv_norm_append_kv")
 
 
 def speechkv_compressed_len(prefix_len: int, speech_len: int, suffix_len: int, w: int,
