@@ -22,35 +22,6 @@ static_assert(32 * kMaskWords >= SPEECHKV_MAX_TREE_NODES && kCommitPath >= SPEEC
 // so many of them reach further; those calls are checked by their own numbers.)
 constexpr int32_t kMaxTreeLen = INT32_MAX - 8191;
 
-// Whether a region of one list overlaps a region of another (null ones take no
-// part).  Lists that lie apart as a whole, as pools and lengths mostly do, are
-// not compared pair by pair.
-template <typename A, typename B>
-bool meet(int na, const A& a, int nb, const B& b) {
-  uintptr_t a_lo = UINTPTR_MAX, a_hi = 0, b_lo = UINTPTR_MAX, b_hi = 0;
-  for (int i = 0; i < na; ++i) {
-    const Region x = a(i);
-    if (!x.p) continue;
-    a_lo = std::min(a_lo, (uintptr_t)x.p);
-    a_hi = std::max(a_hi, (uintptr_t)x.p + (uintptr_t)x.n);
-  }
-  for (int i = 0; i < nb; ++i) {
-    const Region x = b(i);
-    if (!x.p) continue;
-    b_lo = std::min(b_lo, (uintptr_t)x.p);
-    b_hi = std::max(b_hi, (uintptr_t)x.p + (uintptr_t)x.n);
-  }
-  if (a_hi <= b_lo || b_hi <= a_lo) return false;
-  for (int i = 0; i < na; ++i) {
-    const Region x = a(i);
-    for (int j = 0; x.p && j < nb; ++j) {
-      const Region y = b(j);
-      if (y.p && overlaps(x.p, x.n, y.p, y.n)) return true;
-    }
-  }
-  return false;
-}
-
 // How speechkv_tree_attn cuts a call: row groups of a block (1, 2 or 4, of 32
 // rows each) and splits of the keys.
 struct TreePlan {

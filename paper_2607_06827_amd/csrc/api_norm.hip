@@ -3,10 +3,7 @@
 // first HIP call.
 #include "../../include/speechkv_norm.h"
 
-#include <algorithm>
-#include <utility>
-
-#include "host_checks.hpp"
+#include "head_views.hpp"
 #include "kernels_norm.hpp"
 
 namespace {
@@ -15,74 +12,6 @@ using namespace skv;
 
 constexpr int kMaxAxes = 16;
 constexpr float kLeastEps = 1.17549435e-38f;  // 2^-126
-
-// The sizes that the views of a call share.
-struct Sizes {
-  int32_t batch, rows, dim, esz;
-};
-
-// A strided tensor of a call; null data takes no part.
-struct View {
-  const void* p = nullptr;
-  int64_t sb = 0, ss = 0, sh = 0, bytes = 0;
-  int32_t heads = 0;
-};
-
-// Fills v from h; what a written one's axes overlap is refused.
-int view_of_heads(const speechkv_heads* h, const Sizes& n, bool written, View& v) {
-  if (!h) return SPEECHKV_OK;
-  const int64_t per16 = 16 / n.esz;
-  if (!h->data || !aligned16(h->data) || h->num_heads < 1 || h->num_heads > kMaxGrid) return SPEECHKV_ERR_INVALID_ARG;
-  if (bad_stride(h->stride_b, per16) || bad_stride(h->stride_s, per16) || bad_stride(h->stride_h, per16))
-    return SPEECHKV_ERR_INVALID_ARG;
-  const int64_t bytes = extent(n.batch, h->stride_b, n.rows, h->stride_s, h->num_heads, h->stride_h, n.dim, n.esz);
-  if (bytes < 0) return SPEECHKV_ERR_INVALID_ARG;
-  if (written) {
-    std::pair<int64_t, int32_t> axis[3] = {
-        {h->stride_b, n.batch}, {h->stride_s, n.rows}, {h->stride_h, h->num_heads}};
-    std::sort(axis, axis + 3);
-    int64_t span = n.dim;  // (fits: it is at most the extent)
-    for (const auto& [stride, length] : axis) {
-      if (length == 1) continue;
-      if (stride < span) return SPEECHKV_ERR_INVALID_ARG;
-      span += stride * (length - 1);
-    }
-  }
-  v.p = h->data;
-  v.sb = h->stride_b;
-  v.ss = h->stride_s;
-  v.sh = h->stride_h;
-  v.bytes = bytes;
-  v.heads = h->num_heads;
-  return SPEECHKV_OK;
-}
-
-// One tensor with one set of strides (those of axes of length 1 do not matter).
-bool same(const View& a, const View& b, const Sizes& n) {
-  return a.p == b.p && a.heads == b.heads && (n.batch == 1 || a.sb == b.sb) && (n.rows == 1 || a.ss == b.ss) &&
-         (a.heads == 1 || a.sh == b.sh);
-}
-
-// Views whose byte ranges meet but whose rows do not: the heads of each row of b
-// lie behind those of the same row of a, before a's next row.
-bool beside(const View& a, const View& b, const Sizes& n) {
-  if ((n.batch > 1 && a.sb != b.sb) || (n.rows > 1 && a.ss != b.ss)) return false;
-  const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
-  if (off < 0 || off % n.esz) return false;
-  const int64_t d = off / n.esz, span_a = (a.heads - 1) * a.sh + n.dim, span_b = (b.heads - 1) * b.sh + n.dim;
-  const int64_t row = d + span_b;  // what a row of both takes
-  if (d < span_a) return false;
-  if (n.rows > 1 && row > a.ss) return false;
-  return n.batch == 1 || (n.rows > 1 ? (n.rows - 1) * a.ss : 0) + row <= a.sb;
-}
-
-bool clash(const View& a, const View& b, const Sizes& n) {
-  return a.p && b.p && overlaps(a.p, a.bytes, b.p, b.bytes) && !beside(a, b, n) && !beside(b, a, n);
-}
-
-Region region(const View& v) { return {v.p, v.bytes}; }
-
-HeadRows rows_of(const View& v) { return {const_cast<void*>(v.p), v.sb, v.ss, v.sh}; }
 
 int check_sizes(int32_t batch, int32_t rows, const int32_t* row_len) {
   if (batch < 1 || batch > kMaxGrid || rows < 1 || !aligned4(row_len)) return SPEECHKV_ERR_INVALID_ARG;

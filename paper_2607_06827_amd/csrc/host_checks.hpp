@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "common.hpp"
 
 namespace skv {
@@ -97,6 +99,35 @@ inline bool aliased(const Region* wr, int nw, const Region* rd, int nr) {
       if (rd[k].p && overlaps(wr[i].p, wr[i].n, rd[k].p, rd[k].n)) return true;
     for (int k = i + 1; k < nw; ++k)
       if (wr[k].p && overlaps(wr[i].p, wr[i].n, wr[k].p, wr[k].n)) return true;
+  }
+  return false;
+}
+
+// Whether a region of one list overlaps a region of another (null ones take no
+// part).  Lists that lie apart as a whole, as pools and lengths mostly do, are
+// not compared pair by pair.
+template <typename A, typename B>
+bool meet(int na, const A& a, int nb, const B& b) {
+  uintptr_t a_lo = UINTPTR_MAX, a_hi = 0, b_lo = UINTPTR_MAX, b_hi = 0;
+  for (int i = 0; i < na; ++i) {
+    const Region x = a(i);
+    if (!x.p) continue;
+    a_lo = std::min(a_lo, (uintptr_t)x.p);
+    a_hi = std::max(a_hi, (uintptr_t)x.p + (uintptr_t)x.n);
+  }
+  for (int i = 0; i < nb; ++i) {
+    const Region x = b(i);
+    if (!x.p) continue;
+    b_lo = std::min(b_lo, (uintptr_t)x.p);
+    b_hi = std::max(b_hi, (uintptr_t)x.p + (uintptr_t)x.n);
+  }
+  if (a_hi <= b_lo || b_hi <= a_lo) return false;
+  for (int i = 0; i < na; ++i) {
+    const Region x = a(i);
+    for (int j = 0; x.p && j < nb; ++j) {
+      const Region y = b(j);
+      if (y.p && overlaps(x.p, x.n, y.p, y.n)) return true;
+    }
   }
   return false;
 }

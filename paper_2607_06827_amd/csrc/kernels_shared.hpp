@@ -1,0 +1,93 @@
+// Internal interface between the C-ABI host layer and the kernels of shared
+// prefixes, entry weights and eviction (include/speechkv_shared.h).
+#pragma once
+
+#include "kernels_norm.hpp"
+
+namespace skv {
+
+// A cache that is only read: pools, block table and lengths.
+struct KeySource {
+  const void* k_pages;
+  const void* v_pages;
+  const int32_t* table;
+  const int32_t* len;
+  int max_len;  // host bound on len
+  PagedView pv;
+};
+
+struct SharedArgs {
+  const void* q;
+  KeySource prefix, own;       // prefix: rows of table and len by group, own: by sequence
+  const int32_t* group_start;  // [groups + 1]
+  int batch, groups, max_group;
+  int num_q_heads, group_shift;  // log2 of the query heads per KV head
+  float scale_log2;              // scale * log2(e)
+  int row_groups;                // of a prefix block: 1, 2 or 4 (of 32 rows each)
+  int row_tiles;                 // prefix blocks that share a (group, KV head)'s rows
+  int prefix_splits, own_splits;
+  int prefix_tiles, own_tiles;   // key tiles of a split, from the host's bounds
+  int prefix_blocks;             // (set by the launcher, as the divisors)
+  FastDivide by_row_tiles, by_prefix_splits, by_own_splits, by_heads;
+  void* out;
+  float* lse;    // may be null
+  float* ws_o;   // [B][Hq][prefix_splits + own_splits][D] unnormalised partial outputs
+  float* ws_ml;  // [B][Hq][prefix_splits + own_splits][2] running max (log2 units) and sum
+};
+
+struct WeightArgs {
+  HeadRows q;
+  int num_rows;
+  int group_shift;
+  const float* lse;
+  int64_t lse_b, lse_h, lse_s;
+  const int32_t* visible;  // may be null: the rows are the last tokens
+  KeySource cache;         // (no values)
+  int batch;
+  float scale_log2;
+  const float* weights;  // may be null: zeros
+  float* weights_out;
+  int capacity;
+  int row_tiles;   // tiles of 16 rows of a (sequence, KV head)
+  int key_blocks;  // blocks of a (sequence, KV head)
+  FastDivide by_key_blocks, by_heads;  // (set by the launcher)
+};
+constexpr int kWeightKeys = 64;  // keys that a wave holds
+// Row tiles from which the waves of a block share its keys and deal the rows out.
+constexpr int kWeightDealt = 4;
+inline int64_t weight_key_blocks(int max_len, int row_tiles) {
+  const int keys = row_tiles >= kWeightDealt ? kWeightKeys : 4 * kWeightKeys;
+  return ((int64_t)max_len + keys - 1) / keys;
+}
+
+// Layers of one launch of the eviction's kernels: their descriptions travel as
+// kernel arguments (4 KB at most).
+constexpr int kEvictLayers = 32;
+struct EvictLayer {
+  void* k_pages;
+  void* v_pages;
+  const int32_t* table;
+  const int32_t* cache_len;
+  int32_t* cache_len_out;  // may be null
+  const float* weights;
+  float* weights_out;
+  int32_t* kept;
+  int32_t num_pages, page_shift, max_pages;
+};
+struct EvictArgs {
+  EvictLayer layer[kEvictLayers];
+  const int32_t* keep_len;
+  int max_keep, capacity, num_first, num_recent;
+  int kv_heads;
+  int parts;  // column parts of a row (set by the launcher)
+};
+static_assert(sizeof(EvictArgs) <= 4096, "kernel arguments");
+
+// dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
+hipError_t launch_shared(const SharedArgs& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_shared_merge(const SharedArgs& a, int dtype, int head_dim, hipStream_t s);
+constexpr int kSharedKeys = 32;  // keys of a tile
+hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_evict(const EvictArgs& a, int dtype, int head_dim, int layers, int batch, hipStream_t s);
+
+}  // namespace skv

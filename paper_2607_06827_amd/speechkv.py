@@ -1,5 +1,5 @@
-"""ctypes binding of libspeechkv.so (include/speechkv.h, speechkv_draft.h and
-speechkv_norm.h), same names as the C ABI.
+"""ctypes binding of libspeechkv.so (include/speechkv.h, speechkv_draft.h,
+speechkv_norm.h and speechkv_shared.h), same names as the C ABI.
 
 Argument marshalling only: tensors become device pointers, strides and sizes
 become integers, and a non-zero status becomes a SpeechKVError.  Every step of
@@ -41,6 +41,7 @@ MAX_SEGMENTS = 1024  # most segments one sequence of a segment table may have
 NOALLOC_SCRATCH_BYTES = 16 << 20  # static split scratch of speechkv_decode_attn_noalloc, per GPU
 MAX_TREE_NODES = 1024  # most new tokens per sequence of speechkv_tree_attn and speechkv_tree_commit
 MAX_COMMIT_LAYERS = 256  # most layers of one speechkv_tree_commit
+MAX_EVICT_LAYERS = 256  # most layers of one speechkv_evict
 ROPE_HALVES = 0  # elements (j, j + rot_dim / 2) of a head turn together
 ROPE_PAIRS = 1  # elements (2 j, 2 j + 1)
 
@@ -71,6 +72,11 @@ class _LayerCache(ctypes.Structure):
     _fields_ = [("cache", _PagedKV), ("cache_len", ctypes.c_void_p), ("cache_len_out", ctypes.c_void_p)]
 
 
+class _EvictLayer(ctypes.Structure):
+    _fields_ = [("cache", _PagedKV), ("cache_len", ctypes.c_void_p), ("cache_len_out", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("weights_out", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
+
+
 class _Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_s", ctypes.c_int64),
                 ("stride_h", ctypes.c_int64), ("num_heads", ctypes.c_int32)]
@@ -94,6 +100,7 @@ _pack_paged_kv = struct.Struct("@PPPiiiiii").pack
 _pack_spans = struct.Struct("@PPPii").pack
 _pack_segments = struct.Struct("@PPPiii4x").pack  # (padded to the structure's 8-byte alignment)
 _pack_lens = struct.Struct("@PP").pack  # what follows the cache in a layer of a CacheStack
+_pack_evict = struct.Struct("@PPPPP").pack  # what follows the cache in a layer of an EvictStack
 _pack_heads = struct.Struct("@Pqqqi4x").pack
 _pack_norm = struct.Struct("@PPf4x").pack
 _pack_rope = struct.Struct("@PPPiii4x").pack
@@ -179,6 +186,18 @@ _lib.speechkv_norm_rope_bwd_workspace_bytes.argtypes = [_i32] * 5
 _lib.speechkv_norm_rope_bwd_workspace_bytes.restype = _sz
 _lib.speechkv_norm_append_kv.argtypes = [_vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.speechkv_norm_append_kv.restype = ctypes.c_int
+_lib.speechkv_shared_attn.argtypes = [_vp, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _i32, _f32, _i32,
+                                      _vp, _vp, _vp, _sz, _vp]
+_lib.speechkv_shared_attn.restype = ctypes.c_int
+_lib.speechkv_shared_num_splits.argtypes = [_i32] * 9
+_lib.speechkv_shared_num_splits.restype = _i32
+_lib.speechkv_shared_workspace_bytes.argtypes = [_i32] * 9
+_lib.speechkv_shared_workspace_bytes.restype = _sz
+_lib.speechkv_attn_weights.argtypes = [_vp, _i32, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i32, _f32, _vp, _vp,
+                                       _i32, _vp]
+_lib.speechkv_attn_weights.restype = ctypes.c_int
+_lib.speechkv_evict.argtypes = [_vp, _i32, _i32, _vp, _i32, _i32, _i32, _i32, _vp]
+_lib.speechkv_evict.restype = ctypes.c_int
 _lib.speechkv_compressed_len.argtypes = [_i32] * 6
 _lib.speechkv_compressed_len.restype = _i64
 _lib.speechkv_decode_num_splits.argtypes = [_i32, _i32, _i32]
@@ -362,6 +381,50 @@ class CacheStack:
         self._packed = b"".join(packed)
 
 
+class EvictStack:
+    """The caches of a model's layers with the weights of their entries, for
+    speechkv_evict: caches is a list of PagedKV; cache_lens and cache_lens_out
+    are lists of device int32 [B] tensors (cache_lens_out or entries of it may
+    be None), weights and weights_out of fp32 [B, Hkv, capacity] tensors (a
+    layer's may be one tensor) and kept of int32 [B, Hkv, max_keep] tensors, of
+    one size for all layers.  Made once for a set of tensors and kept beside
+    them; it keeps them alive."""
+
+    def __init__(self, caches, cache_lens, cache_lens_out, weights, weights_out, kept):
+        if cache_lens_out is None:
+            cache_lens_out = [None] * len(caches)
+        lists = (cache_lens, cache_lens_out, weights, weights_out, kept)
+        if any(len(x) != len(caches) for x in lists):
+            raise ValueError("one entry of each list per cache")
+        packed = []
+        self._keep = []
+        self.num_layers = len(caches)
+        self.batch = caches[0].block_table.shape[0] if caches else 0
+        self.capacity = weights[0].shape[-1] if caches else 0
+        self.max_keep = kept[0].shape[-1] if caches else 0
+        self.device = caches[0].k_pages.get_device() if caches else -1
+        for c, n, n_out, w, w_out, k in zip(caches, *lists):
+            head = c._paged_kv()
+            rows = (c.block_table.shape[0], c.k_pages.shape[1])
+            if rows[0] != self.batch:
+                raise ValueError("every layer must have the same batch")
+            for x in (n,) if n_out is None else (n, n_out):
+                if x.dtype != torch.int32 or x.shape != (self.batch,) or not x.is_contiguous():
+                    raise ValueError("cache lengths must be contiguous int32 [batch] tensors")
+            for x in (w, w_out):
+                if x.dtype != torch.float32 or x.shape != rows + (self.capacity,) or not x.is_contiguous():
+                    raise ValueError("weights must be contiguous fp32 [batch, heads, capacity] tensors of one size")
+            if k.dtype != torch.int32 or k.shape != rows + (self.max_keep,) or not k.is_contiguous():
+                raise ValueError("kept must be contiguous int32 [batch, heads, max_keep] tensors of one size")
+            tensors = (c.k_pages, c.v_pages, c.block_table, n, w, w_out, k) + (() if n_out is None else (n_out,))
+            if any(x.get_device() != self.device for x in tensors):
+                raise ValueError("every tensor must be on one device")
+            packed.append(head + _pack_evict(n.data_ptr(), 0 if n_out is None else n_out.data_ptr(), w.data_ptr(),
+                                             w_out.data_ptr(), k.data_ptr()))
+            self._keep.append(tensors)
+        self._packed = b"".join(packed)
+
+
 _DTYPE_CODES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
 
 
@@ -388,12 +451,28 @@ def _int32_ptr(x: torch.Tensor, count: int, name: str) -> int:
     return x.data_ptr()
 
 
-def _workspace(x: Optional[torch.Tensor]):
+def _on(device: int, *tensors) -> None:
+    """Refuses tensors of another device than `device`."""
+    for x in tensors:
+        if x is not None and x.get_device() != device:
+            raise ValueError("every tensor of a call must be on one device")
+
+
+def _stream_of(device: int, stream) -> int:
+    """The stream of a call whose tensors are on `device`, which is to be the
+    current one."""
+    if device >= 0 and device != _current_device():
+        raise ValueError("the tensors must be on the current device")
+    return _stream(stream)
+
+
+def _workspace(x: Optional[torch.Tensor], device: int):
     """Address and bytes of a workspace, (None, 0) without one."""
     if x is None:
         return None, 0
     if not x.is_contiguous():
         raise ValueError("the workspace must be contiguous")
+    _on(device, x)
     return x.data_ptr(), x.numel() * x.element_size()
 
 
@@ -822,14 +901,14 @@ def tree_mask(parents, device="cuda") -> torch.Tensor:
 
 
 def _heads(x: Optional[torch.Tensor], rows, dtype) -> Optional[bytes]:
-    """The packed description of rows [B, S, H, D]; rows is (B, S, D)."""
+    """The packed description of rows [B, S, H, D]; rows is (B, S, D, device)."""
     if x is None:
         return None
     shape, strides = x.shape, x.stride()
     if len(shape) != 4 or strides[3] != 1:
         raise ValueError("queries, keys and values must be [B, S, H, D] with a contiguous last axis")
-    if (shape[0], shape[1], shape[3]) != rows or x.dtype != dtype:
-        raise ValueError("queries, keys and values must share batch, rows, head_dim and dtype")
+    if (shape[0], shape[1], shape[3], x.get_device()) != rows or x.dtype != dtype:
+        raise ValueError("queries, keys and values must share batch, rows, head_dim, dtype and device")
     return _pack_heads(x.data_ptr(), strides[0], strides[1], strides[2], _int32(shape[2]))
 
 
@@ -839,6 +918,7 @@ def _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise):
         if g is not None and (g.dtype != torch.float32 or g.numel() != rows[2] or not g.is_contiguous() or
                               not normalise):
             raise ValueError("gamma_q and gamma_k are contiguous fp32 [head_dim] tensors, of a norm")
+    _on(rows[3], gamma_q, gamma_k, row_len)
     norm = _pack_norm(0 if gamma_q is None else gamma_q.data_ptr(), 0 if gamma_k is None else gamma_k.data_ptr(),
                       eps) if normalise else None
     if rope is not None:
@@ -846,6 +926,7 @@ def _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise):
             raise TypeError(f"{type(rope).__name__} given where the call takes a Rope")
         if rope.rows != rows[:2]:
             raise ValueError("the rotation's positions must be of the call's batch and rows")
+        _on(rows[3], *rope._keep)
         rope = rope._packed
     return norm, rope, None if row_len is None else _int32_ptr(row_len, rows[0], "row_len")
 
@@ -862,11 +943,12 @@ def speechkv_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_o
     if x is None or len(x.shape) != 4:
         raise ValueError("q or k must be given, as [B, S, H, D]")
     B, S, _, D = x.shape
-    rows, dt = (B, S, D), x.dtype
+    dev = x.get_device()
+    rows, dt = (B, S, D, dev), x.dtype
     norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
     st = _lib.speechkv_norm_rope(_heads(q, rows, dt), _heads(k, rows, dt), _int32(B), _int32(S), count, _int32(D),
                                  _dtype_code(dt), norm, turn, _heads(q_out, rows, dt), _heads(k_out, rows, dt),
-                                 _stream(stream))
+                                 _stream_of(dev, stream))
     _check(st, "speechkv_norm_rope")
 
 
@@ -889,16 +971,18 @@ def speechkv_norm_rope_bwd(q: Optional[torch.Tensor], k: Optional[torch.Tensor],
     if x is None or len(x.shape) != 4:
         raise ValueError("q or k must be given, as [B, S, H, D]")
     B, S, _, D = x.shape
-    rows, dt = (B, S, D), x.dtype
+    dev = x.get_device()
+    rows, dt = (B, S, D, dev), x.dtype
     norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
     for g in (dgamma_q, dgamma_k):
         if g is not None and (g.dtype != torch.float32 or g.numel() != D or not g.is_contiguous()):
             raise ValueError("dgamma_q and dgamma_k are contiguous fp32 [head_dim] tensors")
-    ws, ws_bytes = _workspace(workspace)
+    _on(dev, dgamma_q, dgamma_k)
+    ws, ws_bytes = _workspace(workspace, dev)
     st = _lib.speechkv_norm_rope_bwd(_heads(q, rows, dt), _heads(k, rows, dt), _heads(dq_out, rows, dt),
                                      _heads(dk_out, rows, dt), _int32(B), _int32(S), count, _int32(D),
                                      _dtype_code(dt), norm, turn, _heads(dq, rows, dt), _heads(dk, rows, dt),
-                                     _ptr(dgamma_q), _ptr(dgamma_k), ws, ws_bytes, _stream(stream))
+                                     _ptr(dgamma_q), _ptr(dgamma_k), ws, ws_bytes, _stream_of(dev, stream))
     _check(st, "speechkv_norm_rope_bwd")
 
 
@@ -914,17 +998,145 @@ def speechkv_norm_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch
     if len(k.shape) != 4:
         raise ValueError("k must be [B, S, Hkv, D]")
     B, S, _, D = k.shape
-    rows, dt = (B, S, D), k.dtype
+    dev = k.get_device()
+    rows, dt = (B, S, D, dev), k.dtype
     c, pages, batch = cache._paged_kv_for(dt)
     if pages[3] != D or batch != B:
         raise ValueError("k and v must have the cache's head_dim and batch")
+    _on(dev, cache.k_pages, cache.v_pages, cache.block_table, cache_len, cache_len_out)
     norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, new_len, normalise)
     lens = _int32_ptr(cache_len, B, "cache_len")
     lens_out = None if cache_len_out is None else _int32_ptr(cache_len_out, B, "cache_len_out")
     st = _lib.speechkv_norm_append_kv(_heads(q, rows, dt), _heads(k, rows, dt), _heads(v, rows, dt), _int32(B),
                                       _int32(S), count, norm, turn, lens, c, _heads(q_out, rows, dt), lens_out,
-                                      _stream(stream))
+                                      _stream_of(dev, stream))
     _check(st, "speechkv_norm_append_kv")
+
+
+def speechkv_shared_attn(q: torch.Tensor, prefix: PagedKV, prefix_len: torch.Tensor, max_prefix_len: int,
+                         group_start: torch.Tensor, max_group: int, cache: PagedKV, cache_len: torch.Tensor,
+                         max_cache_len: int, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None, num_splits: int = 0,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, out: [B, Hq, D] contiguous; prefix: the prefixes' cache, a row of its
+    block table a group; prefix_len: int32 [groups]; group_start: int32 [groups
+    + 1]; cache, cache_len: the sequences' own entries, int32 [B]; lse: fp32
+    [B, Hq] or None; workspace: device bytes, at least
+    speechkv_shared_workspace_bytes(...)."""
+    shape, dt, dev = q.shape, q.dtype, q.get_device()
+    if len(shape) != 3 or out.shape != shape or not q.is_contiguous() or not out.is_contiguous():
+        raise ValueError("q and out must be contiguous [B, Hq, D] tensors of one shape")
+    B, Hq, D = shape
+    c, pages, batch = cache._paged_kv_for(dt)
+    p, prefix_pages, groups = prefix._paged_kv_for(dt)
+    if out.dtype != dt or pages[3] != D or batch != B:
+        raise ValueError("q and out must have the cache's dtype, head_dim and batch")
+    if prefix_pages[1] != pages[1] or prefix_pages[3] != D:
+        raise ValueError("prefix and cache must have the same heads and head_dim")
+    lens, prefix_lens = _int32_ptr(cache_len, B, "cache_len"), _int32_ptr(prefix_len, groups, "prefix_len")
+    starts = _int32_ptr(group_start, groups + 1, "group_start")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, Hq) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous fp32 [B, Hq] tensor")
+    _on(dev, out, cache.k_pages, cache.v_pages, cache.block_table, prefix.k_pages, prefix.v_pages, prefix.block_table,
+        cache_len, prefix_len, group_start, lse)
+    if scale is None:
+        scale = D ** -0.5
+    ws, ws_bytes = _workspace(workspace, dev)
+    st = _lib.speechkv_shared_attn(q.data_ptr(), _int32(B), _int32(Hq), p, prefix_lens, _int32(max_prefix_len), starts,
+                                   _int32(groups), _int32(max_group), c, lens, _int32(max_cache_len), scale,
+                                   num_splits and _int32(num_splits), out.data_ptr(), _ptr(lse), ws, ws_bytes,
+                                   _stream_of(dev, stream))
+    _check(st, "speechkv_shared_attn")
+
+
+def speechkv_shared_num_splits(batch: int, num_groups: int, max_group: int, num_q_heads: int, num_kv_heads: int,
+                               head_dim: int, dtype: torch.dtype, max_prefix_len: int, max_cache_len: int) -> int:
+    return int(_lib.speechkv_shared_num_splits(batch, num_groups, max_group, num_q_heads, num_kv_heads, head_dim,
+                                               _dtype_code(dtype), max_prefix_len, max_cache_len))
+
+
+def speechkv_shared_workspace_bytes(batch: int, num_groups: int, max_group: int, num_q_heads: int, num_kv_heads: int,
+                                    head_dim: int, max_prefix_len: int, max_cache_len: int,
+                                    num_splits: int = 0) -> int:
+    return int(_lib.speechkv_shared_workspace_bytes(batch, num_groups, max_group, num_q_heads, num_kv_heads, head_dim,
+                                                    max_prefix_len, max_cache_len, num_splits))
+
+
+def speechkv_attn_weights(q: torch.Tensor, lse: torch.Tensor, cache: PagedKV, cache_len: torch.Tensor,
+                          max_cache_len: int, weights_out: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                          visible: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                          stream=None) -> None:
+    """q: [B, n, Hq, D] view with a contiguous last axis; lse: fp32 [B, Hq, n]
+    view; weights, weights_out: fp32 [B, Hkv, capacity] contiguous (weights may
+    be weights_out, or None: zeros); visible: int32 [B, n], the entries that
+    each row sees (see visible_slots()), or None: the rows are the sequence's
+    last n tokens."""
+    dt, dev = q.dtype, q.get_device()
+    if len(q.shape) != 4:
+        raise ValueError("q must be [B, n, Hq, D]")
+    B, n, Hq, D = q.shape
+    c, pages, batch = cache._paged_kv_for(dt)
+    if pages[3] != D or batch != B:
+        raise ValueError("q must have the cache's dtype, head_dim and batch")
+    if lse.dtype != torch.float32 or lse.shape != (B, Hq, n):
+        raise ValueError("lse must be an fp32 [B, Hq, n] tensor")
+    for w in (weights_out,) if weights is None else (weights_out, weights):
+        if w.dtype != torch.float32 or len(w.shape) != 3 or w.shape[:2] != (B, pages[1]) or \
+                w.shape != weights_out.shape or not w.is_contiguous():
+            raise ValueError("weights must be contiguous fp32 [B, Hkv, capacity] tensors of one size")
+    lens = _int32_ptr(cache_len, B, "cache_len")
+    seen = None
+    if visible is not None:
+        if visible.dtype != _INT32 or visible.shape != (B, n) or not visible.is_contiguous():
+            raise ValueError("visible must be a contiguous int32 [B, n] tensor")
+        seen = visible.data_ptr()
+    _on(dev, lse, cache.k_pages, cache.v_pages, cache.block_table, cache_len, weights_out, weights, visible)
+    if scale is None:
+        scale = D ** -0.5
+    sb, sh, ss = lse.stride()
+    st = _lib.speechkv_attn_weights(_heads(q, (B, n, D, dev), dt), _int32(B), _int32(n), lse.data_ptr(), sb, sh, ss,
+                                    seen, c, lens, _int32(max_cache_len), scale, _ptr(weights),
+                                    weights_out.data_ptr(), _int32(weights_out.shape[2]), _stream_of(dev, stream))
+    _check(st, "speechkv_attn_weights")
+
+
+def visible_slots(segs, w: int, layer: int, l0: int, mask_mode: int = MASK_WINDOW_END,
+                  device="cuda") -> torch.Tensor:
+    """How many cache entries each row of a prompt sees, for
+    speechkv_attn_weights with the queries and lse of speechkv_prefill_attn:
+    segs is [[(text_len, speech_len), ...] per sequence] ([P | T | N] is [(P, T),
+    (N, 0)]); returns int32 [B, longest], 0 behind a sequence's last row."""
+    w = w if layer >= l0 else 1
+    rows = []
+    for seq in segs:
+        seen, slots = [], 0
+        for text, speech in seq:
+            seen += range(slots + 1, slots + text + 1)
+            slots += text
+            if mask_mode == MASK_WINDOW_START:
+                seen += (slots + t // w + 1 for t in range(speech))
+            else:
+                seen += (slots + (t + 1) // w for t in range(speech))
+                if speech:
+                    seen[-1] = slots + -(-speech // w)
+            slots += -(-speech // w)
+        rows.append(seen)
+    longest = max(map(len, rows), default=0)
+    return torch.tensor([r + [0] * (longest - len(r)) for r in rows], dtype=torch.int32, device=device)
+
+
+def speechkv_evict(layers: EvictStack, keep_len: torch.Tensor, num_first: int, num_recent: int, stream=None) -> None:
+    """keep_len: int32 [B], entries that each sequence keeps; num_first and
+    num_recent of them are its first and its last."""
+    if not isinstance(layers, EvictStack):
+        raise TypeError(f"{type(layers).__name__} given where the call takes an EvictStack")
+    B = layers.batch
+    keep = _int32_ptr(keep_len, B, "keep_len")
+    _on(layers.device, keep_len)
+    st = _lib.speechkv_evict(layers._packed, layers.num_layers, _int32(B), keep, _int32(layers.max_keep),
+                             _int32(layers.capacity), _int32(num_first), _int32(num_recent),
+                             _stream_of(layers.device, stream))
+    _check(st, "speechkv_evict")
 
 
 def speechkv_compressed_len(prefix_len: int, speech_len: int, suffix_len: int, w: int,

@@ -233,7 +233,7 @@ def test_binding_refuses_rotations_and_other_descriptions():
 def test_packed_descriptions_fill_their_structures():
     a, i = host()
     q = a["q"][:, :, 1:3]
-    h = skv._Heads.from_buffer_copy(skv._heads(q, (2, 3, 64), torch.bfloat16))
+    h = skv._Heads.from_buffer_copy(skv._heads(q, (2, 3, 64, -1), torch.bfloat16))
     assert (h.data, h.stride_b, h.stride_s, h.stride_h, h.num_heads) == (q.data_ptr(), 768, 256, 64, 2)
     r = skv.Rope(i(3, 2, 3), torch.zeros(8), i(8), skv.ROPE_PAIRS)
     s = skv._Rope.from_buffer_copy(r._packed)
