@@ -108,7 +108,7 @@ size_t speechkv_norm_rope_bwd_workspace_bytes(int32_t batch, int32_t num_rows, i
   if (check_sizes(batch, num_rows, nullptr) || (head_dim != 64 && head_dim != 128) || num_q_heads < 0 ||
       num_kv_heads < 0 || num_q_heads > kMaxGrid || num_kv_heads > kMaxGrid || num_q_heads + num_kv_heads == 0)
     return 0;
-  return (size_t)norm_bwd_blocks(batch * num_rows) * 2 * head_dim * sizeof(float);
+  return (size_t)norm_bwd_blocks(batch * num_rows, num_q_heads, num_kv_heads, head_dim) * head_dim * sizeof(float);
 }
 
 int speechkv_norm_rope_bwd(const speechkv_heads* q, const speechkv_heads* k, const speechkv_heads* dq_out,
@@ -133,7 +133,9 @@ int speechkv_norm_rope_bwd(const speechkv_heads* q, const speechkv_heads* k, con
   NormArgs a = {};
   Region rd[kPlanRegions + 4];
   if ((st = check_plan(norm, rope, row_len, n, a, rd))) return st;
-  const size_t need = dgamma_q || dgamma_k ? (size_t)norm_bwd_blocks(a.tokens) * 2 * head_dim * sizeof(float) : 0;
+  const size_t need = dgamma_q || dgamma_k ? (size_t)norm_bwd_blocks(a.tokens, in[0].heads, in[1].heads, head_dim) *
+                                                 head_dim * sizeof(float)
+                                           : 0;
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return SPEECHKV_ERR_WORKSPACE;
   for (int x = 0; x < 2; ++x) {
     if (in[x].heads != grad[x].heads || in[x].heads != out[x].heads) return SPEECHKV_ERR_INVALID_ARG;
@@ -160,13 +162,9 @@ int speechkv_norm_rope_bwd(const speechkv_heads* q, const speechkv_heads* k, con
   a.q_heads = in[0].heads;
   a.k_heads = in[1].heads;
   a.partial = need ? static_cast<float*>(workspace) : nullptr;
-  a.blocks = norm_bwd_blocks(a.tokens);
   a.dgamma_q = dgamma_q;
   a.dgamma_k = dgamma_k;
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_norm_bwd(a, dtype, head_dim, s);
-  if (e == hipSuccess && need) e = launch_norm_gamma(a, head_dim, s);
-  return status_of(e);
+  return status_of(launch_norm_bwd(a, dtype, head_dim, static_cast<hipStream_t>(stream)));
 }
 
 int speechkv_norm_append_kv(const speechkv_heads* q, const speechkv_heads* k, const speechkv_heads* v, int32_t batch,

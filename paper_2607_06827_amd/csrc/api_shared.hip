@@ -173,15 +173,17 @@ int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_ro
   if (lse_bytes < 0) return SPEECHKV_ERR_INVALID_ARG;
   WeightArgs a = {};
   a.row_tiles = (int)(((int64_t)num_rows * group + 15) / 16);
-  const int64_t key_blocks = weight_key_blocks(max_cache_len, a.row_tiles);
-  if (((__int128)batch * heads + 7) * key_blocks > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
+  a.batch = batch;
+  a.cache = source_of(cache, cache_len, max_cache_len);
+  plan_weights(a, n.dim * n.esz);
+  if (((__int128)batch * heads + 7) * a.key_blocks > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4, sums = lens * heads * capacity;
   const Region rd[] = {{vq.p, vq.bytes}, {lse, lse_bytes}, {visible, lens * num_rows}, {cache_len, lens},
                        {cache->block_table, table_bytes(cache, batch)}, {cache->k_pages, pool},
                        {weights == weights_out ? nullptr : weights, sums}};
   const Region wr[] = {{weights_out, sums}};
   if (aliased(wr, 1, rd, 7)) return SPEECHKV_ERR_ALIAS;
-  if (key_blocks == 0) return SPEECHKV_OK;  // (no entries)
+  if (max_cache_len == 0) return SPEECHKV_OK;  // (no entries)
   a.q = rows_of(vq);
   a.num_rows = num_rows;
   a.group_shift = log2_exact(group);
@@ -190,13 +192,10 @@ int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_ro
   a.lse_h = lse_stride_h;
   a.lse_s = lse_stride_s;
   a.visible = visible;
-  a.cache = source_of(cache, cache_len, max_cache_len);
-  a.batch = batch;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.weights = weights;
   a.weights_out = weights_out;
   a.capacity = capacity;
-  a.key_blocks = (int)key_blocks;
   return status_of(launch_weights(a, cache->dtype, cache->head_dim, static_cast<hipStream_t>(stream)));
 }
 

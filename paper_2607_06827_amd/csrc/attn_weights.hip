@@ -1,18 +1,21 @@
 // The attention weight that cache entries gather from queries: for entry c the sum
 // of exp(scale q.k_c - lse) over the rows that see it, added to what it has.
 //
-// A wave holds 64 keys of a (sequence, KV head) in registers (four tiles of 16,
-// operand A) and goes through the rows, query heads of the group and queries, in
-// tiles of 16 (operand B): S^T = K Q^T on the 16x16 matrix products, the weights
-// straight from it, summed per key in a lane's own registers; the 16 lanes of a
-// key add up once, at the end.  Keys and rows go from memory into the operands
-// (a lane's 16-byte pieces; four lanes read 64 bytes of a row): K is read once and
-// never needed in LDS.  The order of the elements along a row is that of the
-// pieces, for both operands alike.
+// S^T = K Q^T on the 16x16 matrix products (operand A: 16 keys, B: 16 rows, the
+// query heads of the group and queries), the weights straight from it, summed per
+// key in a lane's own registers over the rows; the 16 lanes of a key add up once,
+// at the end.  Keys and rows come through LDS by direct loads of whole rows:
+// loaded straight into the operands, whose neighbouring lanes hold different rows,
+// every 16 bytes are an access of their own (128 cycles an instruction of 64 lanes
+// instead of 16; the prompts of 8 users 59 us).  16-byte chunks of a row are
+// swizzled by the row so that operand reads are spread over the banks.
 //
-// With few row tiles (a decoding step) every wave has keys of its own; with more
-// the waves of a block share 64 keys, deal the row tiles out and add up through
-// LDS, in order.
+// Few rows (a decoding step): the rows stay in LDS and each wave streams keys of its
+// own, 32 a step, one step ahead.  Bound by reading the keys.
+// Many rows (a prompt): a block holds 64 keys in its waves' registers, the waves deal
+// the row tiles out, each streaming those of its own, and add up through LDS.
+#include <algorithm>
+
 #include "attn_mfma.hpp"
 #include "kernels_shared.hpp"
 
@@ -20,9 +23,49 @@ namespace skv {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTiles = kWeightKeys / 16;
-constexpr int kSpreadUnits = 32;  // pairs from which an XCD keeps a pair's blocks together
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kSpreadUnits = 32;  // pairs from which an XCD takes pairs of its own
+
+// Rows of 16-byte chunks in LDS: chunk c of row r at position c ^ swizzle(r).
+template <typename T, int D>
+struct Rows16 {
+  static constexpr int kBytes = D * (int)sizeof(T);  // of a row
+  static constexpr int kChunks = kBytes / 16;
+  static constexpr int kPieces = kChunks / 4;         // 16-byte pieces of a row per lane
+  static constexpr int kPerLoad = 64 / kChunks;       // rows of a direct load
+  static constexpr int kTileLoads = 16 / kPerLoad;    // direct loads of 16 rows
+  static constexpr int kTileBytes = 16 * kBytes;
+  static __device__ __forceinline__ int swizzle(int row) { return kChunks == 8 ? (row >> 1) & 7 : row & 15; }
+  // pieces of row `col` of the 16 rows at `lds`: chunks 4 p + quarter
+  static __device__ __forceinline__ void read(u32x4_t (&x)[kPieces], uint32_t lds, int col, int quarter) {
+    typedef __attribute__((address_space(3))) const u32x4_t* lds_ptr;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p)
+      x[p] = *(lds_ptr)(uintptr_t)(lds + col * kBytes + (((4 * p + quarter) ^ swizzle(col)) << 4));
+  }
+};
+
+// 16 bytes per lane from the per-lane address p into LDS at lds + 16 * lane,
+// untracked like lds_dma16; kOnce: without keeping the line in the caches.
+template <bool kOnce>
+__device__ __forceinline__ void lds_dma16_from(const void* p, uint32_t lds) {
+  if constexpr (kOnce)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(p), "s"(lds) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+}
+
+template <int kVm>
+__device__ __forceinline__ void wait_vm() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0)" : : "i"(kVm) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 template <typename T>
 __device__ __forceinline__ f32x4_t product(u32x4_t k, u32x4_t q, f32x4_t c) {
@@ -37,17 +80,24 @@ __device__ __forceinline__ f32x4_t product(u32x4_t k, u32x4_t q, f32x4_t c) {
   }
 }
 
-// v[j] summed over the 16 lanes of a row, for j = the lane's number in the row.
-__device__ __forceinline__ float transposed_sum(float (&v)[16], int lane) {
+// v[j] summed over the 16 lanes of a row, for j = the lane's number in the row
+// (mod the number of values).
+template <int n>
+__device__ __forceinline__ float transposed_sum(float (&v)[n], int lane) {
   auto step = [&](auto half, auto ctrl) __attribute__((always_inline)) {
-    constexpr int n = decltype(half)::value;
-    const bool up = lane & n;
+    constexpr int m = decltype(half)::value;
+    const bool up = lane & m;
 #pragma unroll
-    for (int k = 0; k < n; ++k) {
-      const float keep = up ? v[k + n] : v[k], send = up ? v[k] : v[k + n];
-      v[k] = keep + dpp<decltype(ctrl)::value>(send);
+    for (int k = 0; k < m; ++k) {
+      if constexpr (m < n) {
+        const float keep = up ? v[k + m] : v[k], send = up ? v[k] : v[k + m];
+        v[k] = keep + dpp<decltype(ctrl)::value>(send);
+      } else {
+        v[k] += dpp<decltype(ctrl)::value>(v[k]);
+      }
     }
   };
+  static_assert(n == 8 || n == 16, "values of a lane");
   step(std::integral_constant<int, 8>(), std::integral_constant<int, kDppRowRor8>());
   step(std::integral_constant<int, 4>(), std::integral_constant<int, kDppHalfMirror>());
   step(std::integral_constant<int, 2>(), std::integral_constant<int, kDppQuadXor2>());
@@ -55,95 +105,324 @@ __device__ __forceinline__ float transposed_sum(float (&v)[16], int lane) {
   return v[0];
 }
 
-// kDealt: the waves of a block share its keys and deal the row tiles out.
-template <typename T, int D, bool kDealt>
-__global__ __launch_bounds__(kThreads, 2) void weights_kernel(WeightArgs a) {
-  constexpr int kPieces = D * (int)sizeof(T) / 64;  // 16-byte pieces of a row per lane
-  constexpr int kElems = 16 / (int)sizeof(T);       // of a piece
-  __shared__ float s_part[kWaves][kWeightKeys];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 15, quarter = lane >> 4;
+// A block's (sequence, KV head) and its number among that pair's blocks.
+struct Unit {
+  int pair, part, b, g, len;
+};
+__device__ __forceinline__ bool unit_of(const WeightArgs& a, Unit& u) {
   const int heads = a.cache.pv.kv_heads, pairs = a.batch * heads;
-  int pair, part, b, g;
+  // An XCD (block index mod 8) takes neighbouring pairs: the KV heads of a
+  // sequence, whose rows lie beside each other.
   if (pairs >= kSpreadUnits) {
-    a.by_key_blocks.divide((int)(blockIdx.x >> 3), pair, part);
-    pair = pair * 8 + (blockIdx.x & 7);
-    if (pair >= pairs) return;
+    const int per = (pairs + 7) / 8;
+    a.by_key_blocks.divide((int)(blockIdx.x >> 3), u.pair, u.part);
+    if (u.pair >= per) return false;
+    u.pair += (int)(blockIdx.x & 7) * per;
+    if (u.pair >= pairs) return false;
   } else {
-    a.by_key_blocks.divide((int)blockIdx.x, pair, part);
+    a.by_key_blocks.divide((int)blockIdx.x, u.pair, u.part);
   }
-  a.by_heads.divide(pair, b, g);
+  a.by_heads.divide(u.pair, u.b, u.g);
   const PagedView& pv = a.cache.pv;
-  const int len = (int)min((int64_t)min(max(a.cache.len[b], 0), a.cache.max_len), (int64_t)pv.max_pages << pv.page_shift);
-  const int kb = kDealt ? part * kWeightKeys : (part * kWaves + wave) * kWeightKeys;
-  if (kb >= len) return;
+  u.len = (int)min((int64_t)min(max(a.cache.len[u.b], 0), a.cache.max_len), (int64_t)pv.max_pages << pv.page_shift);
+  return true;
+}
 
-  // the keys: lane (col, quarter) has pieces quarter, 4 + quarter, .. of key col of each tile
-  u32x4_t k[kTiles][kPieces];
-  uint64_t present = 0;  // keys that exist and have a page
-  {
-    const int32_t* table = a.cache.table + (int64_t)b * pv.max_pages;
-    const T* pool = static_cast<const T*>(a.cache.k_pages);
+// Direct loads of 16 n keys from key kb on into LDS at `to`, by one wave (which
+// takes every `share`-th load); keys behind the last read the last, keys without a
+// page rows of page 0.  `entry`: lane lane0 + i has the block-table entry of the
+// 2^kRun keys from kb + 2^kRun i on (or of the last).
+template <typename T, int D, int kTiles, int kRun, bool kOnce>
+__device__ __forceinline__ void load_keys(const WeightArgs& a, const Unit& u, int kb, int entry, int lane0, uint32_t to,
+                                          int lane, int first, int share) {
+  typedef Rows16<T, D> L;
+  const PagedView& pv = a.cache.pv;
+  const int lrow = lane / L::kChunks, lpos = lane % L::kChunks;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int key = min(kb + 16 * t + col, len - 1);
-      const int64_t page = table[key >> pv.page_shift];
-      const bool ok = page >= 0 && page < pv.num_pages;
-      const T* row = pool + page_row<D>(ok ? page : 0, g, key & ((1 << pv.page_shift) - 1), pv) + quarter * kElems;
-      const uint64_t there = __builtin_amdgcn_ballot_w64(ok && kb + 16 * t + col < len);
-      present |= (there & 0xffffu) << (16 * t);
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p) k[t][p] = *reinterpret_cast<const u32x4_t*>(row + 4 * p * kElems);
-    }
+  for (int n = 0; n < kTiles * L::kTileLoads; ++n) {
+    if (share > 1 && n % share != first) continue;
+    const int row = n * L::kPerLoad + lrow, key = min(kb + row, u.len - 1);
+    const int e = __shfl(entry, lane0 + ((key - kb) >> kRun), 64);
+    const int64_t page = e >= 0 && e < pv.num_pages ? e : 0;
+    const char* from = static_cast<const char*>(a.cache.k_pages) +
+                       page_row<D>(page, u.g, key & ((1 << pv.page_shift) - 1), pv) * (int)sizeof(T) +
+                       ((lpos ^ L::swizzle(row)) << 4);
+    lds_dma16_from<kOnce>(from, __builtin_amdgcn_readfirstlane(to + n * 1024));
   }
+}
 
-  float sum[16];  // element 4 t + i: key 16 t + 4 quarter + i, over this lane's rows
+// Address of row r (0 .. 15) of row tile rt, query head r % G of the tile's query
+// r / G; rows behind the last read query 0.
+template <typename T>
+__device__ __forceinline__ const char* row_of(const WeightArgs& a, const Unit& u, int rt, int r) {
+  const int i = rt * (16 >> a.group_shift) + (r >> a.group_shift);
+  const int h = (u.g << a.group_shift) + (r & ((1 << a.group_shift) - 1));
+  return reinterpret_cast<const char*>(static_cast<const T*>(a.q.p) + u.b * a.q.sb + (i < a.num_rows ? i : 0) * a.q.ss +
+                                       h * a.q.sh);
+}
+
+// Direct loads of row tile rt into LDS at `to`, by one wave.
+template <typename T, int D>
+__device__ __forceinline__ void load_rows(const WeightArgs& a, const Unit& u, int rt, uint32_t to, int lane) {
+  typedef Rows16<T, D> L;
+  const int lrow = lane / L::kChunks, lpos = lane % L::kChunks;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) sum[j] = 0.f;
-  const int gmask = (1 << a.group_shift) - 1, rows = a.num_rows << a.group_shift;
-  const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + quarter * kElems;
-  const float* lse = a.lse + b * a.lse_b;
-  for (int rt = kDealt ? wave : 0; rt < a.row_tiles; rt += kDealt ? kWaves : 1) {
-    const int r = rt * 16 + col;
-    const int i = min(r, rows - 1) >> a.group_shift, h = (g << a.group_shift) + (r & gmask);
-    int seen = a.visible ? a.visible[(int64_t)b * a.num_rows + i] : len - (a.num_rows - 1 - i);
-    seen = r < rows ? min(max(seen, 0), len) : 0;
-    if (!__builtin_amdgcn_ballot_w64(seen > kb)) continue;
-    const float l = lse[h * a.lse_h + i * a.lse_s] * 1.4426950408889634f;
-    if (l == neg_inf()) seen = 0;  // (a row that saw nothing)
-    const T* row = q + i * a.q.ss + h * a.q.sh;
-    u32x4_t x[kPieces];
+  for (int n = 0; n < L::kTileLoads; ++n) {
+    const int row = n * L::kPerLoad + lrow;
+    lds_dma16_from<false>(row_of<T>(a, u, rt, row) + ((lpos ^ L::swizzle(row)) << 4),
+                          __builtin_amdgcn_readfirstlane(to + n * 1024));
+  }
+}
+
+// Where this lane's row of tile rt has its lse and its number of seen entries.
+__device__ __forceinline__ const float* lse_of(const WeightArgs& a, const Unit& u, int rt, int col) {
+  const int i = rt * (16 >> a.group_shift) + (col >> a.group_shift);
+  const int h = (u.g << a.group_shift) + (col & ((1 << a.group_shift) - 1));
+  return a.lse + u.b * a.lse_b + h * a.lse_h + (i < a.num_rows ? i : 0) * a.lse_s;
+}
+__device__ __forceinline__ const int32_t* seen_at(const WeightArgs& a, const Unit& u, int i) {
+  // (without a list the length: a load that no branch depends on)
+  return a.visible ? a.visible + (int64_t)u.b * a.num_rows + (i < a.num_rows ? i : 0) : a.cache.len + u.b;
+}
+// What query i sees, of what the list says.
+__device__ __forceinline__ int seen_of(const WeightArgs& a, const Unit& u, int n, int i) {
+  if (!a.visible) n = u.len - (a.num_rows - 1 - i);
+  return i < a.num_rows ? min(max(n, 0), u.len) : 0;
+}
+
+// Adds the weights that 16 rows x give the keys k (16 a tile, from key kb on): sum
+// element 4 t + e is of key 16 t + 4 quarter + e, over this lane's rows.
+template <typename T, int D, int kTiles>
+__device__ __forceinline__ void add_rows(const WeightArgs& a, const u32x4_t (&k)[kTiles][Rows16<T, D>::kPieces],
+                                         const u32x4_t (&x)[Rows16<T, D>::kPieces], float lse, int seen, int kb,
+                                         int quarter, float (&sum)[4 * kTiles]) {
+  const float l = lse * 1.4426950408889634f;
+  if (l == neg_inf()) seen = 0;  // (a row that saw nothing)
+  f32x4_t st[kTiles];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) x[p] = *reinterpret_cast<const u32x4_t*>(row + 4 * p * kElems);
-    const bool all = !__builtin_amdgcn_ballot_w64(seen < kb + kWeightKeys);
+  for (int t = 0; t < kTiles; ++t) st[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // (the tiles' sums in turn: a product waits for the one before it of its sum)
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      f32x4_t st = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < Rows16<T, D>::kPieces; ++p)
 #pragma unroll
-      for (int p = 0; p < kPieces; ++p) st = product<T>(k[t][p], x[p], st);
+    for (int t = 0; t < kTiles; ++t) st[t] = product<T>(k[t][p], x[p], st[t]);
+  if (!__builtin_amdgcn_ballot_w64(seen < kb + 16 * kTiles)) {  // every row sees all keys
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[4 * t + e] += fast_exp2(__builtin_fmaf(st[t][e], a.scale_log2, -l));
+  } else {
+    const int most = seen - kb - 4 * quarter;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float w = fast_exp2(__builtin_fmaf(st[e], a.scale_log2, -l));
-        const int key = kb + 16 * t + 4 * quarter + e;
-        sum[4 * t + e] += all || key < seen ? w : 0.f;
+        const float w = fast_exp2(__builtin_fmaf(st[t][e], a.scale_log2, -l));
+        sum[4 * t + e] += 16 * t + e < most ? w : 0.f;
+      }
+  }
+}
+
+// Key (of 16 kTiles) whose total transposed_sum leaves in this lane.
+template <int kTiles>
+__device__ __forceinline__ int key_of(int col, int quarter) {
+  return 16 * ((col >> 2) & (kTiles - 1)) + 4 * quarter + (col & 3);
+}
+
+// ---------------------------------------------------------------- few rows
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void weights_few_kernel(WeightArgs a) {
+  typedef Rows16<T, D> L;
+  constexpr int kTiles = kWeightStep / 16, kStepBytes = kTiles * L::kTileBytes, kN = kTiles * L::kTileLoads;
+  __shared__ __attribute__((aligned(1024))) unsigned char s_q[kWeightFew * L::kTileBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[kWaves][2][kStepBytes];
+  __shared__ float s_sum[kWaves * kWeightSteps * kWeightStep];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  Unit u;
+  if (!unit_of(a, u)) return;
+  // a block has a stretch of keys, its waves steps of 32 of it in turn
+  const int block_keys = kWaves * a.steps * kWeightStep, k0 = u.part * block_keys;
+  if (k0 >= u.len) return;
+  const int steps = min(a.steps, max((u.len - k0 + kWeightStep - 1) / kWeightStep - wave + kWaves - 1, 0) / kWaves);
+  auto key0 = [&](int step) { return k0 + (step * kWaves + wave) * kWeightStep; };
+  const int32_t* table = a.cache.table + (int64_t)u.b * a.cache.pv.max_pages;
+  // lane 4 s + i has the table entry of keys 8 i .. of step s (pages hold at least 8)
+  static_assert(kWeightSteps * kWeightStep / 8 <= 64 && kWeightStep == 32, "a lane for every 8 keys");
+  int entry = table[min(key0(lane >> 2) + 8 * (lane & 3), u.len - 1) >> a.cache.pv.page_shift];
+  // the rows' lse and what they see; all of it has arrived before the first direct
+  // load of a key, which the compiler does not count
+  float l[kWeightFew];
+  int seen[kWeightFew];
+#pragma unroll
+  for (int rt = 0; rt < kWeightFew; ++rt) {
+    const int i = rt * (16 >> a.group_shift) + (col >> a.group_shift);
+    l[rt] = *lse_of(a, u, rt, col);
+    seen[rt] = seen_of(a, u, *seen_at(a, u, i), i);
+  }
+  const uint32_t sq = lds_addr(s_q), sk = lds_addr(s_k[wave]);
+  for (int rt = wave; rt < a.row_tiles; rt += kWaves) load_rows<T, D>(a, u, rt, sq + rt * L::kTileBytes, lane);
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+#pragma unroll
+  for (int rt = 0; rt < kWeightFew; ++rt) asm volatile("" : "+v"(l[rt]), "+v"(seen[rt]));
+  asm volatile("" : "+v"(entry));
+  __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();  // the rows are in LDS
+
+  const uint64_t pages = __builtin_amdgcn_ballot_w64(entry >= 0 && entry < a.cache.pv.num_pages);
+  // (always: what waits for the others counts on it; behind the last step the keys
+  // of the last one again)
+  auto request = [&](int step) __attribute__((always_inline)) {
+    const int s = min(step, max(steps - 1, 0));
+    load_keys<T, D, kTiles, 3, true>(a, u, key0(s), entry, 4 * s, sk + (step & 1) * kStepBytes, lane, 0, 1);
+  };
+  request(0);
+  request(1);
+  for (int step = 0; step < steps; ++step) {
+    const int kb = key0(step);
+    const uint32_t ok = ((((uint32_t)(pages >> (4 * step)) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu;  // a byte each
+    wait_vm<kN>();
+    u32x4_t k[kTiles][L::kPieces];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) L::read(k[t], sk + (step & 1) * kStepBytes + t * L::kTileBytes, col, quarter);
+    wait_lds();
+    request(step + 2);
+    float sum[4 * kTiles];
+#pragma unroll
+    for (int j = 0; j < 4 * kTiles; ++j) sum[j] = 0.f;
+#pragma unroll
+    for (int rt = 0; rt < kWeightFew; ++rt)
+      if (rt < a.row_tiles) {
+        u32x4_t x[L::kPieces];
+        L::read(x, sq + rt * L::kTileBytes, col, quarter);
+        add_rows<T, D, kTiles>(a, k, x, l[rt], seen[rt], kb, quarter, sum);
+      }
+    const float total = transposed_sum(sum, lane);
+    const int at = key_of<kTiles>(col, quarter);
+    s_sum[(step * kWaves + wave) * kWeightStep + at] = ok >> at & 1 ? total : 0.f;
+  }
+  wait_vm<0>();
+  __syncthreads();
+  const int64_t row = (int64_t)u.pair * a.capacity + k0;
+  for (int c = tid; c < min(block_keys, u.len - k0); c += kThreads)
+    a.weights_out[row + c] = (a.weights ? a.weights[row + c] : 0.f) + s_sum[c];
+}
+
+// --------------------------------------------------------------- many rows
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a) {
+  typedef Rows16<T, D> L;
+  constexpr int kKeys = weight_keys(L::kBytes), kTiles = kKeys / 16;
+  constexpr int kAhead = L::kBytes > 256 ? 2 : 4;  // row tiles of a wave on their way
+  constexpr int kN = L::kTileLoads + 2;            // direct loads of a row tile
+  __shared__ __attribute__((aligned(1024))) unsigned char s_row[kWaves][kAhead][L::kTileBytes];
+  __shared__ float s_lse[kWaves][kAhead][64];
+  __shared__ int s_seen[kWaves][kAhead][64];
+  __shared__ float s_part[kWaves][kKeys];
+  __shared__ uint64_t s_sees[kWaves];
+  static_assert(sizeof(s_row) >= kTiles * L::kTileBytes, "the keys come through the rows' place");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  Unit u;
+  if (!unit_of(a, u)) return;
+  const int kb = u.part * kKeys;
+  if (kb >= u.len) return;
+
+  u32x4_t k[kTiles][L::kPieces];
+  uint64_t present;  // keys that have a page
+  {
+    const int32_t* table = a.cache.table + (int64_t)u.b * a.cache.pv.max_pages;
+    const int entry = table[min(kb + lane, u.len - 1) >> a.cache.pv.page_shift];
+    present = __builtin_amdgcn_ballot_w64(entry >= 0 && entry < a.cache.pv.num_pages);
+    const uint32_t sk = lds_addr(s_row);
+    load_keys<T, D, kTiles, 0, false>(a, u, kb, entry, 0, sk, lane, wave, kWaves);
+    wait_vm<0>();
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) L::read(k[t], sk + t * L::kTileBytes, col, quarter);
+    wait_lds();
+    __syncthreads();  // the keys are in registers: rows take their place
+  }
+
+  float sum[4 * kTiles];
+#pragma unroll
+  for (int j = 0; j < 4 * kTiles; ++j) sum[j] = 0.f;
+  const int queries = 16 >> a.group_shift, in = col >> a.group_shift;
+  const uint32_t s_rows = lds_addr(s_row[wave]), s_lses = lds_addr(s_lse[wave]), s_seens = lds_addr(s_seen[wave]);
+  auto request = [&](int rt, int buffer) __attribute__((always_inline)) {
+    load_rows<T, D>(a, u, rt, s_rows + buffer * L::kTileBytes, lane);
+    lds_dma4(lse_of(a, u, rt, col), __builtin_amdgcn_readfirstlane(s_lses + buffer * 256));
+    lds_dma4(seen_at(a, u, rt * queries + in), __builtin_amdgcn_readfirstlane(s_seens + buffer * 256));
+  };
+
+  // kWaves * 64 row tiles at a time, 64 a wave: lane n finds out whether any row of
+  // tile n sees these keys.  Every wave then goes through those tiles of its own (one
+  // in kWaves) that do, kAhead of them requested ahead.  From the last row to the
+  // first: in a prompt the last rows see most, so the blocks of a sequence read the
+  // same rows at the same time, out of one L2.
+  constexpr uint64_t kMine = 0x1111111111111111ull;
+  static_assert(kWaves == 4, "tiles of a wave");
+  for (int rt0 = (a.row_tiles - 1) / (64 * kWaves) * (64 * kWaves); rt0 >= 0; rt0 -= 64 * kWaves) {
+    int most = 0;
+#pragma unroll 8
+    for (int n = 0; n < queries; ++n) {
+      const int i = (rt0 + 64 * wave + lane) * queries + n;
+      most = max(most, seen_of(a, u, *seen_at(a, u, i), i));
+    }
+    const uint64_t sees = __builtin_amdgcn_ballot_w64(most > kb);
+    __syncthreads();  // (the last masks have been read)
+    if (lane == 0) s_sees[wave] = sees;
+    __syncthreads();
+    int count = 0, word = kWaves;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) count += __builtin_popcountll(s_sees[w] & (kMine << wave));
+    count = __builtin_amdgcn_readfirstlane(count);
+    if (!count) continue;
+    uint64_t todo = 0;
+    int last = rt0;
+    auto next = [&]() {  // the wave's next tile, the last one again behind it
+      while (!todo && word > 0) {
+        --word;
+        const uint64_t x = s_sees[word] & (kMine << wave);
+        todo = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 |
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x);
+      }
+      if (todo) {
+        const int bit = 63 - __builtin_clzll(todo);
+        todo ^= (uint64_t)1 << bit;
+        last = rt0 + 64 * word + bit;
+      }
+      return last;
+    };
+    int tile[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) request(tile[j] = next(), j);
+    for (int at = 0; at < count; at += kAhead) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        wait_vm<(kAhead - 1) * kN>();
+        u32x4_t x[L::kPieces];
+        L::read(x, s_rows + j * L::kTileBytes, col, quarter);
+        const float l = s_lse[wave][j][lane];
+        const int seen = seen_of(a, u, s_seen[wave][j][lane], tile[j] * queries + in);
+        wait_lds();
+        request(tile[j] = next(), j);  // (always: what waits for the others counts on it)
+        if (at + j < count) add_rows<T, D, kTiles>(a, k, x, l, seen, kb, quarter, sum);
       }
     }
+    wait_vm<0>();
   }
-  float total = transposed_sum(sum, lane);  // of key 16 (col / 4) + 4 quarter + col % 4
-  int at = 16 * (col >> 2) + 4 * quarter + (col & 3);
-  if constexpr (kDealt) {
-    s_part[wave][at] = total;
-    __syncthreads();
-    if (wave) return;
-    at = lane;
-    total = 0.f;
+  s_part[wave][key_of<kTiles>(col, quarter)] = transposed_sum(sum, lane);
+  __syncthreads();
+  if (tid < kKeys && kb + tid < u.len) {
+    float total = 0.f;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) total += s_part[v][at];
-  }
-  if (kb + at < len) {
-    const int64_t to = (int64_t)pair * a.capacity + kb + at;
-    const float had = a.weights ? a.weights[to] : 0.f;
-    a.weights_out[to] = present >> at & 1 ? had + total : had;
+    for (int v = 0; v < kWaves; ++v) total += s_part[v][tid];
+    const int64_t to = (int64_t)u.pair * a.capacity + kb + tid;
+    a.weights_out[to] = (a.weights ? a.weights[to] : 0.f) + (present >> tid & 1 ? total : 0.f);
   }
 }
 
@@ -156,13 +435,28 @@ hipError_t launch_weights_d(const WeightArgs& args, hipStream_t s) {
   a.by_heads = FastDivide(a.cache.pv.kv_heads);
   const int64_t pairs = (int64_t)a.batch * a.cache.pv.kv_heads;
   const dim3 grid((uint32_t)((pairs >= kSpreadUnits ? (pairs + 7) / 8 * 8 : pairs) * a.key_blocks)), block(kThreads);
-  return a.row_tiles >= kWeightDealt ? launch_struct(weights_kernel<T, D, true>, grid, block, s, a)
-                                     : launch_struct(weights_kernel<T, D, false>, grid, block, s, a);
+  return a.row_tiles > kWeightFew ? launch_struct(weights_many_kernel<T, D>, grid, block, s, a)
+                                  : launch_struct(weights_few_kernel<T, D>, grid, block, s, a);
 }
 
 hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStream_t s) {
   if (dtype == 1) return head_dim == 128 ? launch_weights_d<bf16_bits, 128>(a, s) : launch_weights_d<bf16_bits, 64>(a, s);
   return head_dim == 128 ? launch_weights_d<float, 128>(a, s) : launch_weights_d<float, 64>(a, s);
+}
+
+// Steps of a wave with few rows: what spreads the keys over the blocks that run at
+// once (two a CU), so that they end together.
+void plan_weights(WeightArgs& a, int row_bytes) {
+  const int64_t pairs = (int64_t)a.batch * a.cache.pv.kv_heads;
+  if (a.row_tiles > kWeightFew) {
+    a.steps = 1;
+    a.key_blocks = (int)(((int64_t)a.cache.max_len + weight_keys(row_bytes) - 1) / weight_keys(row_bytes));
+    return;
+  }
+  const int64_t tiles = ((int64_t)a.cache.max_len + kWeightStep - 1) / kWeightStep;
+  const int64_t want = (pairs * tiles + 512 * kWaves - 1) / (512 * kWaves);
+  a.steps = (int)std::max<int64_t>(1, std::min<int64_t>(want, kWeightSteps));
+  a.key_blocks = (int)((tiles + kWaves * a.steps - 1) / (kWaves * a.steps));
 }
 
 }  // namespace skv

@@ -12,8 +12,17 @@ struct HeadRows {
   int64_t sb, ss, sh;
 };
 
-// Most tokens of a block.
+// Most tokens of a wave's step.
 constexpr int kNormTokens = 8;
+
+// How one kind of rows (queries, keys or values) is dealt out: a step of a wave
+// takes the rows of `tokens` tokens, `split` waves share a step, and the kind has
+// `blocks` blocks.
+struct NormPart {
+  int heads;     // 0: there are none
+  int tokens, steps, split, blocks;
+  FastDivide by_heads;
+};
 
 struct NormArgs {
   HeadRows q, k, v;        // inputs (v: appended values)
@@ -21,8 +30,8 @@ struct NormArgs {
   HeadRows dq, dk;         // backward: gradients of the inputs (q_out, k_out: of the outputs)
   int q_heads, k_heads;    // 0: without them
   int num_rows, tokens;    // rows of a sequence, rows in all
-  int per_block;           // tokens of a block (1 .. kNormTokens)
-  FastDivide by_rows, by_q, by_k;  // num_rows, q_heads, k_heads (set by the launcher)
+  FastDivide by_rows;      // num_rows (set by the launcher, as the parts)
+  NormPart part[3];        // queries, keys, values
   const int32_t* row_len;  // may be null: num_rows
   int normalise;
   const float* gamma_q;    // may be null: 1
@@ -42,17 +51,16 @@ struct NormArgs {
   PagedView pv;
   int32_t* cache_len_out;  // may be null
   // backward
-  float* partial;          // [blocks][2][D] sums of dgamma, null: none wanted
-  int blocks;              // that write partial sums
+  float* partial;          // [blocks of the queries, then of the keys][D] sums of dgamma, null: none wanted
   float* dgamma_q;         // may be null
   float* dgamma_k;
 };
 
 // dtype: 0 = fp32, 1 = bf16.  Each launcher returns the launch status.
 hipError_t launch_norm(const NormArgs& a, bool append, int dtype, int head_dim, hipStream_t s);
+// The backward, and with a.partial the sums of dgamma behind it.
 hipError_t launch_norm_bwd(const NormArgs& a, int dtype, int head_dim, hipStream_t s);
-hipError_t launch_norm_gamma(const NormArgs& a, int head_dim, hipStream_t s);
-// Blocks of the backward, by the number of tokens.
-int norm_bwd_blocks(int tokens);
+// Blocks of the backward that write sums of dgamma.
+int norm_bwd_blocks(int tokens, int q_heads, int k_heads, int head_dim);
 
 }  // namespace skv

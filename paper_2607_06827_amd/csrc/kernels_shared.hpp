@@ -49,16 +49,16 @@ struct WeightArgs {
   float* weights_out;
   int capacity;
   int row_tiles;   // tiles of 16 rows of a (sequence, KV head)
+  int steps;       // with few rows: steps of a wave (set by the plan, as key_blocks)
   int key_blocks;  // blocks of a (sequence, KV head)
   FastDivide by_key_blocks, by_heads;  // (set by the launcher)
 };
-constexpr int kWeightKeys = 64;  // keys that a wave holds
-// Row tiles from which the waves of a block share its keys and deal the rows out.
-constexpr int kWeightDealt = 4;
-inline int64_t weight_key_blocks(int max_len, int row_tiles) {
-  const int keys = row_tiles >= kWeightDealt ? kWeightKeys : 4 * kWeightKeys;
-  return ((int64_t)max_len + keys - 1) / keys;
-}
+constexpr int kWeightFew = 2;     // row tiles that a block keeps in LDS
+constexpr int kWeightStep = 32;   // keys of a wave's step with few rows
+constexpr int kWeightSteps = 16;  // most steps of a wave
+// Keys of a block with many rows.
+constexpr int weight_keys(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
+void plan_weights(WeightArgs& a, int row_bytes);
 
 // Layers of one launch of the eviction's kernels: their descriptions travel as
 // kernel arguments (4 KB at most).

@@ -8,12 +8,15 @@
 //
 // A thread holds 16 elements of a row, two 8-element chunks: the two whose
 // elements turn together, or two of the elements that stay.  D / 16 neighbouring
-// lanes hold a row and add their sums with lane exchanges.  A block takes some
-// tokens (rows of q and k of one position): their sines and cosines are computed
-// once, by a thread each, and shared through LDS.  Angles are counted in turns,
-// whose whole part drops out in 64 bits, so that far positions lose nothing.
+// lanes hold a row and add their sums with lane exchanges.  A wave takes the
+// queries (or the keys, or the values) of some tokens and needs no other wave:
+// its lanes work out an angle each, whose sine and cosine the rows share through
+// LDS.  Angles are counted in turns, whose whole part drops out in 64 bits, so that
+// far positions lose nothing.
 //
 // Sums, norms, the rotation and gradients are fp32; each output is rounded once.
+#include <algorithm>
+
 #include "kernels_norm.hpp"
 
 namespace skv {
@@ -74,40 +77,53 @@ __device__ __forceinline__ void turn(float (&u)[8], float (&w)[8], const float2*
   }
 }
 
-// A block's tokens: sequence and row of token t, whether the sequence has it.
-struct Token {
-  int b, i;
-  bool there;
-};
-__device__ __forceinline__ Token token(const NormArgs& a, int t) {
-  const bool in = t < a.tokens;
-  int b, i;
-  a.by_rows.divide(in ? t : 0, b, i);
-  const int n = a.row_len ? a.row_len[b] : a.num_rows;
-  return {b, i, in && i < n};
+// LDS that a wave writes before its own lanes read it.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// (cos, sin) of the angles of the block's tokens, D / 2 apart.
+// A wave's tokens: where the rows of head 0 start in up to three tensors, in
+// elements, and their (cos, sin), D / 2 apart.
 template <int D>
-__device__ __forceinline__ void fill_turns(const NormArgs& a, int first, float2* s_turn) {
-  const int half = a.rot / 2, batch_rows = a.tokens;
-  for (int x = threadIdx.x; x < a.per_block * (D / 2); x += kThreads) {
-    const int j = x % (D / 2), t = first + x / (D / 2);
-    if (j >= half || t >= batch_rows) continue;
-    const Token k = token(a, t);
-    if (!k.there) continue;
-    const int axis = a.axis ? min(max(a.axis[j], 0), a.num_axes - 1) : 0;
-    const double n = (double)a.positions[(int64_t)axis * batch_rows + t] * ((double)a.inv_freq[j] * 0.15915494309189535);
-    float s, c;
-    sincospif(2.f * (float)(n - __builtin_rint(n)), &s, &c);
-    s_turn[x] = make_float2(c, s);
+struct Step {
+  float2 turn[kNormTokens * (D / 2)];
+  int64_t at[3][kNormTokens];
+  int there[kNormTokens];
+};
+
+// Fills the step of tokens first .. first + n: f(token, b, i) gives the three
+// places and whether the token is there.
+template <int D, typename F>
+__device__ __forceinline__ void fill_step(const NormArgs& a, int first, int n, bool turns, int lane, Step<D>& s, F f) {
+  wave_fence();  // (the last step's have been read)
+  if (lane < n) {
+    const int t = first + lane;
+    int b, i;
+    a.by_rows.divide(min(t, a.tokens - 1), b, i);
+    const int rows = a.row_len ? a.row_len[b] : a.num_rows;
+    int64_t at[3] = {0, 0, 0};
+    s.there[lane] = f(t, b, i, t < a.tokens && i < rows, at);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) s.at[x][lane] = at[x];
   }
+  if (turns) {
+    const int j = lane % (D / 2);
+    const bool used = j < a.rot / 2;
+    const double inv = used ? (double)a.inv_freq[j] * 0.15915494309189535 : 0.0;
+    const int axis = used && a.axis ? min(max(a.axis[j], 0), a.num_axes - 1) : 0;
+    for (int in = lane / (D / 2); in < n; in += 64 / (D / 2)) {
+      const int t = min(first + in, a.tokens - 1);
+      const double x = (double)a.positions[(int64_t)axis * a.tokens + t] * inv;
+      float sn, cs;
+      sincospif(2.f * (float)(x - __builtin_rint(x)), &sn, &cs);
+      s.turn[in * (D / 2) + j] = make_float2(cs, sn);
+    }
+  }
+  wave_fence();
 }
 
-template <typename T>
-__device__ __forceinline__ const T* row_at(const HeadRows& x, const Token& k, int h) {
-  return static_cast<const T*>(x.p) + k.b * x.sb + k.i * x.ss + h * x.sh;
-}
+__device__ __forceinline__ int64_t offset_of(const HeadRows& x, int b, int i) { return b * x.sb + i * x.ss; }
 
 __device__ __forceinline__ void load_gamma(float (&x)[8], float (&y)[8], const float* gamma, const Place& at) {
   Chunk<float> c, d;
@@ -130,232 +146,283 @@ __device__ __forceinline__ float inverse_size(const float (&u)[8], const float (
   return 1.f / sqrtf(row_sum<D>(sum) * (1.f / D) + eps);
 }
 
+// Which kind of rows a block has, and its number among those blocks.
+__device__ __forceinline__ int kind_of(const NormArgs& a, int& block) {
+  block = blockIdx.x;
+  for (int kind = 0; kind < 2; ++kind) {
+    if (block < a.part[kind].blocks) return kind;
+    block -= a.part[kind].blocks;
+  }
+  return 2;
+}
+
 // kAppend: keys and values go behind the cache's entries.
 template <typename T, int D, bool kAppend>
 __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
-  constexpr int kLanes = D / 16;  // of a row
-  __shared__ float2 s_turn[kNormTokens * (D / 2)];
-  const int tid = threadIdx.x, first = blockIdx.x * a.per_block;
-  const Place at(tid % kLanes, a);
-  if (a.rot) {
-    fill_turns<D>(a, first, s_turn);
-    __syncthreads();
-  }
-  // what goes where: q rows, k rows and v rows of one token after the other
-  auto move = [&](const T* src, T* dst, const float2* t, const float* gamma, bool plain) {
+  constexpr int kLanes = D / 16, kGroups = 64 / kLanes;  // lanes of a row, rows of a wave
+  __shared__ Step<D> s_step[kThreads / 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int block;
+  const int kind = kind_of(a, block);
+  const NormPart& part = a.part[kind];
+  const int id = block * (kThreads / 64) + wave, step = id / part.split, share = id % part.split;
+  if (step >= part.steps) return;
+  const Place at(lane % kLanes, a);
+  const bool turning = a.rot && kind < 2;
+  Step<D>& s = s_step[wave];
+  const HeadRows& src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+  const bool paged = kAppend && kind > 0;
+  fill_step<D>(a, step * part.tokens, part.tokens, turning, lane, s, [&](int, int b, int i, bool there, int64_t (&to)[3]) {
+    to[0] = offset_of(src, b, i);
+    if (!paged) {
+      to[1] = offset_of(kind ? a.k_out : a.q_out, b, i);
+      return there;
+    }
+    const int len = max(a.cache_len[b], 0);
+    if (kind == 1 && i == 0 && a.cache_len_out) {
+      const int n = a.row_len ? min(max(a.row_len[b], 0), a.num_rows) : a.num_rows;
+      a.cache_len_out[b] = (int32_t)min((int64_t)len + n, (int64_t)INT32_MAX);
+    }
+    const int64_t slot = (int64_t)len + i, index = slot >> a.pv.page_shift;
+    if (!there || index >= a.pv.max_pages) return false;
+    const int64_t page = a.table[(int64_t)b * a.pv.max_pages + index];
+    to[1] = page_row<D>(page, 0, (int)(slot & ((1 << a.pv.page_shift) - 1)), a.pv);
+    return page >= 0 && page < a.pv.num_pages;
+  });
+  T* const out = static_cast<T*>(paged ? (kind == 1 ? a.k_pages : a.v_pages) : kind ? a.k_out.p : a.q_out.p);
+  const int64_t out_head = paged ? (int64_t)D << a.pv.page_shift : kind ? a.k_out.sh : a.q_out.sh;
+  const bool normed = a.normalise && kind < 2, turns = turning && at.turns;
+  const float* gamma = kind ? a.gamma_k : a.gamma_q;
+  for (int r = lane / kLanes + kGroups * share; r < part.tokens * part.heads; r += kGroups * part.split) {
+    int in, h;
+    part.by_heads.divide(r, in, h);
+    if (!s.there[in]) continue;
+    const T* from = static_cast<const T*>(src.p) + s.at[0][in] + h * src.sh;
+    T* dst = out + s.at[1][in] + h * out_head;
     Chunk<T> x, y;
-    load_row(x, src + 8 * at.c0);
-    load_row(y, src + 8 * at.c1);
-    if (!plain && (a.normalise || at.turns)) {
+    load_row(x, from + 8 * at.c0);
+    load_row(y, from + 8 * at.c1);
+    if (normed || turns) {
       float u[8], w[8];
       x.to_float(u);
       y.to_float(w);
-      if (a.normalise) {
-        const float r = inverse_size<D>(u, w, a.eps);
+      if (normed) {
+        const float size = inverse_size<D>(u, w, a.eps);
         float gu[8], gw[8];
         load_gamma(gu, gw, gamma, at);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          u[e] *= r * gu[e];
-          w[e] *= r * gw[e];
+          u[e] *= size * gu[e];
+          w[e] *= size * gw[e];
         }
       }
-      if (at.turns) turn<false>(u, w, t + 8 * at.p, a.pairs);
+      if (turns) turn<false>(u, w, s.turn + in * (D / 2) + 8 * at.p, a.pairs);
       x.from_float(u);
       y.from_float(w);
     }
     x.store(dst + 8 * at.c0);
     y.store(dst + 8 * at.c1);
-  };
-  for (int r = tid / kLanes; r < a.per_block * a.q_heads; r += kThreads / kLanes) {
-    int in, h;
-    a.by_q.divide(r, in, h);
-    const Token k = token(a, first + in);
-    if (!k.there) continue;
-    move(row_at<T>(a.q, k, h), const_cast<T*>(row_at<T>(a.q_out, k, h)), s_turn + in * (D / 2), a.gamma_q, false);
-  }
-  const int k_rows = a.k_heads * (kAppend ? 2 : 1);
-  for (int r = tid / kLanes; r < a.per_block * k_rows; r += kThreads / kLanes) {
-    int in, h;
-    a.by_k.divide(r, in, h);
-    const bool is_v = kAppend && in >= a.per_block;  // (all keys first)
-    if (is_v) in -= a.per_block;
-    const Token k = token(a, first + in);
-    if (!k.there) continue;
-    T* dst;
-    if constexpr (kAppend) {
-      const int64_t slot = (int64_t)max(a.cache_len[k.b], 0) + k.i;
-      const int64_t index = slot >> a.pv.page_shift;
-      if (index >= a.pv.max_pages) continue;
-      const int64_t page = a.table[(int64_t)k.b * a.pv.max_pages + index];
-      if (page < 0 || page >= a.pv.num_pages) continue;
-      dst = static_cast<T*>(is_v ? a.v_pages : a.k_pages) +
-            page_row<D>(page, h, (int)(slot & ((1 << a.pv.page_shift) - 1)), a.pv);
-    } else {
-      dst = const_cast<T*>(row_at<T>(a.k_out, k, h));
-    }
-    move(row_at<T>(is_v ? a.v : a.k, k, h), dst, s_turn + in * (D / 2), a.gamma_k, is_v);
-  }
-  if constexpr (kAppend) {
-    if (a.cache_len_out && tid < a.per_block && first + tid < a.tokens) {
-      int b, i;
-      a.by_rows.divide(first + tid, b, i);
-      const int n = a.row_len ? min(max(a.row_len[b], 0), a.num_rows) : a.num_rows;
-      if (i == 0) a.cache_len_out[b] = (int32_t)min((int64_t)max(a.cache_len[b], 0) + n, (int64_t)INT32_MAX);
-    }
   }
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(NormArgs a) {
-  constexpr int kLanes = D / 16, kGroups = kThreads / kLanes;
-  __shared__ float2 s_turn[kNormTokens * (D / 2)];
-  __shared__ float s_sum[kGroups][D + 4];
-  const int tid = threadIdx.x, group = tid / kLanes;
-  const Place at(tid % kLanes, a);
-  float dgu[2][8] = {}, dgw[2][8] = {};  // this lane's sums of dgamma_q and dgamma_k
-  for (int first = blockIdx.x * a.per_block; first < a.tokens; first += a.blocks * a.per_block) {
-    if (a.rot) {
-      __syncthreads();  // (the last tokens' angles have been read)
-      fill_turns<D>(a, first, s_turn);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const HeadRows &src = kind ? a.k : a.q, &grad = kind ? a.k_out : a.q_out, &to = kind ? a.dk : a.dq;
-      const int heads = kind ? a.k_heads : a.q_heads;
-      float gu[8], gw[8];
-      if (a.normalise) load_gamma(gu, gw, kind ? a.gamma_k : a.gamma_q, at);
-      for (int r = group; r < a.per_block * heads; r += kGroups) {
-        int in, h;
-        (kind ? a.by_k : a.by_q).divide(r, in, h);
-        const Token k = token(a, first + in);
-        if (!k.there) continue;
-        const T* dy = row_at<T>(grad, k, h);
-        Chunk<T> x, y;
-        load_row(x, dy + 8 * at.c0);
-        load_row(y, dy + 8 * at.c1);
-        if (a.normalise || at.turns) {
-          float u[8], w[8];
-          x.to_float(u);
-          y.to_float(w);
-          if (at.turns) turn<true>(u, w, s_turn + in * (D / 2) + 8 * at.p, a.pairs);
-          if (a.normalise) {
-            const T* from = row_at<T>(src, k, h);
-            float xu[8], xw[8];
-            Chunk<T> c;
-            load_row(c, from + 8 * at.c0);
-            c.to_float(xu);
-            load_row(c, from + 8 * at.c1);
-            c.to_float(xw);
-            const float s = inverse_size<D>(xu, xw, a.eps);
-            float dot = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              xu[e] *= s;
-              xw[e] *= s;
-              dgu[kind][e] += u[e] * xu[e];
-              dgw[kind][e] += w[e] * xw[e];
-              u[e] *= gu[e];
-              w[e] *= gw[e];
-              dot += u[e] * xu[e] + w[e] * xw[e];
-            }
-            dot = row_sum<D>(dot) * (1.f / D);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              u[e] = s * (u[e] - xu[e] * dot);
-              w[e] = s * (w[e] - xw[e] * dot);
-            }
-          }
-          x.from_float(u);
-          y.from_float(w);
-        }
-        T* dst = const_cast<T*>(row_at<T>(to, k, h));
-        x.store(dst + 8 * at.c0);
-        y.store(dst + 8 * at.c1);
+  constexpr int kLanes = D / 16, kGroups = 64 / kLanes, kWaves = kThreads / 64;
+  __shared__ Step<D> s_step[kWaves];
+  __shared__ float s_sum[kWaves * kGroups][D + 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int block;
+  const int kind = kind_of(a, block);
+  const NormPart& part = a.part[kind];
+  const Place at(lane % kLanes, a);
+  Step<D>& s = s_step[wave];
+  const HeadRows &src = kind ? a.k : a.q, &grad = kind ? a.k_out : a.q_out, &to = kind ? a.dk : a.dq;
+  float gu[8], gw[8], dgu[8] = {}, dgw[8] = {};  // gamma, this lane's sums of dgamma
+  if (a.normalise) load_gamma(gu, gw, kind ? a.gamma_k : a.gamma_q, at);
+  const bool turns = a.rot && at.turns;
+  for (int id = block * kWaves + wave; id < part.steps * part.split; id += part.blocks * kWaves) {
+    const int step = id / part.split, share = id % part.split;
+    fill_step<D>(a, step * part.tokens, part.tokens, a.rot, lane, s, [&](int, int b, int i, bool there, int64_t (&x)[3]) {
+      x[0] = offset_of(src, b, i);
+      x[1] = offset_of(grad, b, i);
+      x[2] = offset_of(to, b, i);
+      return there;
+    });
+    for (int r = lane / kLanes + kGroups * share; r < part.tokens * part.heads; r += kGroups * part.split) {
+      int in, h;
+      part.by_heads.divide(r, in, h);
+      if (!s.there[in]) continue;
+      const T* dy = static_cast<const T*>(grad.p) + s.at[1][in] + h * grad.sh;
+      const T* from = static_cast<const T*>(src.p) + s.at[0][in] + h * src.sh;
+      T* dst = static_cast<T*>(to.p) + s.at[2][in] + h * to.sh;
+      Chunk<T> x, y, cx, cy;
+      load_row(x, dy + 8 * at.c0);
+      load_row(y, dy + 8 * at.c1);
+      if (a.normalise) {
+        load_row(cx, from + 8 * at.c0);
+        load_row(cy, from + 8 * at.c1);
       }
+      if (a.normalise || turns) {
+        float u[8], w[8];
+        x.to_float(u);
+        y.to_float(w);
+        if (turns) turn<true>(u, w, s.turn + in * (D / 2) + 8 * at.p, a.pairs);
+        if (a.normalise) {
+          float xu[8], xw[8];
+          cx.to_float(xu);
+          cy.to_float(xw);
+          const float size = inverse_size<D>(xu, xw, a.eps);
+          float dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            xu[e] *= size;
+            xw[e] *= size;
+            dgu[e] += u[e] * xu[e];
+            dgw[e] += w[e] * xw[e];
+            u[e] *= gu[e];
+            w[e] *= gw[e];
+            dot += u[e] * xu[e] + w[e] * xw[e];
+          }
+          dot = row_sum<D>(dot) * (1.f / D);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            u[e] = size * (u[e] - xu[e] * dot);
+            w[e] = size * (w[e] - xw[e] * dot);
+          }
+        }
+        x.from_float(u);
+        y.from_float(w);
+      }
+      x.store(dst + 8 * at.c0);
+      y.store(dst + 8 * at.c1);
     }
   }
   if (!a.partial) return;
   // the block's sums, group by group in order
+  const int group = wave * kGroups + lane / kLanes;
 #pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s_sum[group][8 * at.c0 + e] = dgu[kind][e];
-      s_sum[group][8 * at.c1 + e] = dgw[kind][e];
-    }
-    __syncthreads();
-    if (tid < D) {
-      float sum = 0.f;
-      for (int g = 0; g < kGroups; ++g) sum += s_sum[g][tid];
-      a.partial[((int64_t)blockIdx.x * 2 + kind) * D + tid] = sum;
-    }
+  for (int e = 0; e < 8; ++e) {
+    s_sum[group][8 * at.c0 + e] = dgu[e];
+    s_sum[group][8 * at.c1 + e] = dgw[e];
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float sum = 0.f;
+#pragma unroll 8
+    for (int g = 0; g < kWaves * kGroups; ++g) sum += s_sum[g][threadIdx.x];
+    a.partial[(int64_t)blockIdx.x * D + threadIdx.x] = sum;
   }
 }
 
-// dgamma from the blocks' sums, in a fixed order: a block takes 8 elements of one
-// of the two, 32 threads an element.
+// dgamma from the blocks' sums, in a fixed order: a block takes 32 elements of one
+// of the two, 128 threads every four elements.
+constexpr int kGammaThreads = 1024;
 template <int D>
-__global__ __launch_bounds__(kThreads) void norm_gamma_kernel(NormArgs a) {
-  __shared__ float s_sum[32][9];
-  const int kind = blockIdx.x / (D / 8), e = blockIdx.x % (D / 8) * 8 + threadIdx.x % 8, part = threadIdx.x / 8;
+__global__ __launch_bounds__(kGammaThreads) void norm_gamma_kernel(NormArgs a) {
+  constexpr int kParts = kGammaThreads / 8;
+  __shared__ f32x4_t s_sum[kParts][8];
+  const int kind = blockIdx.x / (D / 32), e = threadIdx.x % 8, at = threadIdx.x / 8;
+  const int col = blockIdx.x % (D / 32) * 32 + 4 * e;
   float* to = kind ? a.dgamma_k : a.dgamma_q;
   if (!to) return;
-  float sum = 0.f;
-  for (int n = part; n < a.blocks; n += 32) sum += a.partial[((int64_t)n * 2 + kind) * D + e];
-  s_sum[part][threadIdx.x % 8] = sum;
-  __syncthreads();
-  if (part == 0) {
-    sum = 0.f;
-    for (int n = 0; n < 32; ++n) sum += s_sum[n][threadIdx.x];
-    to[e] = sum;
+  const int first = kind ? a.part[0].blocks : 0, n = a.part[kind].blocks;
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = at; i < n; i += kParts) {
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.partial + (int64_t)(first + i) * D + col);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] += x[k];
+  }
+  s_sum[at][e] = sum;
+#pragma unroll
+  for (int half = kParts / 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (at < half) {
+      const f32x4_t x = s_sum[at + half][e];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[k] += x[k];
+      s_sum[at][e] = sum;
+    }
+  }
+  if (at == 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[col + k] = sum[k];
   }
 }
 
-NormArgs with_divisors(const NormArgs& a) {
-  NormArgs x = a;
-  x.by_rows = FastDivide(a.num_rows);
-  x.by_q = FastDivide(a.q_heads ? a.q_heads : 1);
-  x.by_k = FastDivide(a.k_heads ? a.k_heads : 1);
-  return x;
+// Waves that fill the chip (256 CUs of four SIMDs, some waves each).
+constexpr int kFull = 4096;
+
+// A wave's step: about four rows a lane group, so that the angles are worked out
+// for several rows, but only while the steps fill the chip; with few of them the
+// waves share a step's rows.
+NormPart part_of(int tokens, int heads, int head_dim) {
+  const int groups = 64 / (head_dim / 16);
+  NormPart p;
+  p.heads = heads;
+  p.tokens = 1;
+  p.steps = tokens;
+  p.split = 1;
+  p.blocks = 0;
+  p.by_heads = FastDivide(heads ? heads : 1);
+  if (!heads) return p;
+  while (p.tokens < kNormTokens && p.tokens * heads < 4 * groups && tokens / (2 * p.tokens) >= kFull) p.tokens *= 2;
+  p.steps = (tokens + p.tokens - 1) / p.tokens;
+  if (p.steps < kFull / 2) p.split = (p.tokens * heads + groups - 1) / groups;
+  p.blocks = (int)(((int64_t)p.steps * p.split + kThreads / 64 - 1) / (kThreads / 64));
+  return p;
+}
+
+// Blocks of a part of the backward: those of the forward, but no more than what
+// runs at once (each writes its sums of dgamma), queries and keys by their heads.
+void limit_blocks(NormPart (&p)[3]) {
+  const int64_t heads = p[0].heads + p[1].heads;
+  for (int kind = 0; kind < 2; ++kind)
+    if (p[kind].heads) p[kind].blocks = (int)std::min<int64_t>(p[kind].blocks, 1 + kFull / 4 * (int64_t)p[kind].heads / heads);
 }
 
 }  // namespace
 
-int norm_bwd_blocks(int tokens) { return tokens < 1024 ? tokens : 1024; }
+int norm_bwd_blocks(int tokens, int q_heads, int k_heads, int head_dim) {
+  NormPart p[3] = {part_of(tokens, q_heads, head_dim), part_of(tokens, k_heads, head_dim), part_of(tokens, 0, head_dim)};
+  limit_blocks(p);
+  return p[0].blocks + p[1].blocks;
+}
 
 template <typename T, int D>
-hipError_t launch_norm_d(const NormArgs& a, bool append, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.tokens + a.per_block - 1) / a.per_block)), block(kThreads);
+hipError_t launch_norm_d(const NormArgs& args, bool append, hipStream_t s) {
+  NormArgs a = args;
+  a.by_rows = FastDivide(a.num_rows);
+  a.part[0] = part_of(a.tokens, a.q_heads, D);
+  a.part[1] = part_of(a.tokens, a.k_heads, D);
+  a.part[2] = part_of(a.tokens, append ? a.k_heads : 0, D);
+  const dim3 grid((uint32_t)(a.part[0].blocks + a.part[1].blocks + a.part[2].blocks)), block(kThreads);
   return append ? launch_struct(norm_kernel<T, D, true>, grid, block, s, a)
                 : launch_struct(norm_kernel<T, D, false>, grid, block, s, a);
 }
 
-hipError_t launch_norm(const NormArgs& args, bool append, int dtype, int head_dim, hipStream_t s) {
-  NormArgs a = with_divisors(args);
-  a.per_block = 1;
+hipError_t launch_norm(const NormArgs& a, bool append, int dtype, int head_dim, hipStream_t s) {
   if (dtype == 1) return head_dim == 128 ? launch_norm_d<bf16_bits, 128>(a, append, s) : launch_norm_d<bf16_bits, 64>(a, append, s);
   return head_dim == 128 ? launch_norm_d<float, 128>(a, append, s) : launch_norm_d<float, 64>(a, append, s);
 }
 
-hipError_t launch_norm_bwd(const NormArgs& args, int dtype, int head_dim, hipStream_t s) {
-  NormArgs a = with_divisors(args);
-  a.per_block = 1;
-  const dim3 grid((uint32_t)a.blocks), block(kThreads);
-  if (dtype == 1) {
-    if (head_dim == 128) return launch_struct(norm_bwd_kernel<bf16_bits, 128>, grid, block, s, a);
-    return launch_struct(norm_bwd_kernel<bf16_bits, 64>, grid, block, s, a);
-  }
-  if (head_dim == 128) return launch_struct(norm_bwd_kernel<float, 128>, grid, block, s, a);
-  return launch_struct(norm_bwd_kernel<float, 64>, grid, block, s, a);
+template <typename T, int D>
+hipError_t launch_norm_bwd_d(const NormArgs& args, hipStream_t s) {
+  NormArgs a = args;
+  a.by_rows = FastDivide(a.num_rows);
+  a.part[0] = part_of(a.tokens, a.q_heads, D);
+  a.part[1] = part_of(a.tokens, a.k_heads, D);
+  a.part[2] = part_of(a.tokens, 0, D);
+  limit_blocks(a.part);
+  const dim3 grid((uint32_t)(a.part[0].blocks + a.part[1].blocks)), block(kThreads);
+  const hipError_t e = launch_struct(norm_bwd_kernel<T, D>, grid, block, s, a);
+  if (e != hipSuccess || !a.partial) return e;
+  return launch_struct(norm_gamma_kernel<D>, dim3(2 * D / 32), dim3(kGammaThreads), s, a);
 }
 
-hipError_t launch_norm_gamma(const NormArgs& a, int head_dim, hipStream_t s) {
-  const dim3 grid(2 * head_dim / 8), block(kThreads);
-  return head_dim == 128 ? launch_struct(norm_gamma_kernel<128>, grid, block, s, a)
-                         : launch_struct(norm_gamma_kernel<64>, grid, block, s, a);
+hipError_t launch_norm_bwd(const NormArgs& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 1) return head_dim == 128 ? launch_norm_bwd_d<bf16_bits, 128>(a, s) : launch_norm_bwd_d<bf16_bits, 64>(a, s);
+  return head_dim == 128 ? launch_norm_bwd_d<float, 128>(a, s) : launch_norm_bwd_d<float, 64>(a, s);
 }
 
 }  // namespace skv

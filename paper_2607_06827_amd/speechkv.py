@@ -346,6 +346,9 @@ class Rope:
         if layout not in (ROPE_HALVES, ROPE_PAIRS):
             raise ValueError("layout must be ROPE_HALVES or ROPE_PAIRS")
         self.rows = tuple(positions.shape[-2:])
+        self.device = positions.get_device()
+        if inv_freq.get_device() != self.device or (axis is not None and axis.get_device() != self.device):
+            raise ValueError("every tensor must be on one device")
         self._keep = (positions, inv_freq, axis)
         axes = positions.shape[0] if positions.dim() == 3 else 1
         self._packed = _pack_rope(positions.data_ptr(), inv_freq.data_ptr(), 0 if axis is None else axis.data_ptr(),
@@ -441,7 +444,7 @@ def _int32(n) -> int:
     return n if -2**31 <= operator.index(n) < 2**31 else -1
 
 
-_INT32 = torch.int32
+_INT32, _FLOAT32 = torch.int32, torch.float32
 
 
 def _int32_ptr(x: torch.Tensor, count: int, name: str) -> int:
@@ -451,11 +454,17 @@ def _int32_ptr(x: torch.Tensor, count: int, name: str) -> int:
     return x.data_ptr()
 
 
-def _on(device: int, *tensors) -> None:
-    """Refuses tensors of another device than `device`."""
-    for x in tensors:
-        if x is not None and x.get_device() != device:
-            raise ValueError("every tensor of a call must be on one device")
+def _cache_on(cache: PagedKV, dev: int) -> bool:
+    return cache.k_pages.get_device() == cache.v_pages.get_device() == cache.block_table.get_device() == dev
+
+
+def _counts(x: Optional[torch.Tensor], count: int, dev: int, name: str) -> Optional[int]:
+    """Address of contiguous int32 values on a device, None without them."""
+    if x is None:
+        return None
+    if x.dtype != _INT32 or x.numel() != count or not x.is_contiguous() or x.get_device() != dev:
+        raise ValueError(f"{name} must be a contiguous int32 tensor with one value for each")
+    return x.data_ptr()
 
 
 def _stream_of(device: int, stream) -> int:
@@ -470,9 +479,8 @@ def _workspace(x: Optional[torch.Tensor], device: int):
     """Address and bytes of a workspace, (None, 0) without one."""
     if x is None:
         return None, 0
-    if not x.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
-    _on(device, x)
+    if not x.is_contiguous() or x.get_device() != device:
+        raise ValueError("the workspace must be contiguous and on the call's device")
     return x.data_ptr(), x.numel() * x.element_size()
 
 
@@ -900,35 +908,57 @@ def tree_mask(parents, device="cuda") -> torch.Tensor:
     return torch.tensor(rows, dtype=torch.int32, device=device)
 
 
-def _heads(x: Optional[torch.Tensor], rows, dtype) -> Optional[bytes]:
-    """The packed description of rows [B, S, H, D]; rows is (B, S, D, device)."""
+def _heads(x: Optional[torch.Tensor], B: int, S: int, D: int, dtype, dev: int) -> Optional[bytes]:
+    """The packed description of rows [B, S, H, D] of one dtype and device."""
     if x is None:
         return None
-    shape, strides = x.shape, x.stride()
-    if len(shape) != 4 or strides[3] != 1:
-        raise ValueError("queries, keys and values must be [B, S, H, D] with a contiguous last axis")
-    if (shape[0], shape[1], shape[3], x.get_device()) != rows or x.dtype != dtype:
-        raise ValueError("queries, keys and values must share batch, rows, head_dim, dtype and device")
-    return _pack_heads(x.data_ptr(), strides[0], strides[1], strides[2], _int32(shape[2]))
+    b, s, h, d = x.shape
+    sb, ss, sh, se = x.stride()
+    if se != 1 or b != B or s != S or d != D or x.dtype != dtype or x.get_device() != dev:
+        raise ValueError("queries, keys and values must be [B, S, H, D] with a contiguous last axis, of one batch, "
+                         "rows, head_dim, dtype and device")
+    try:
+        return _pack_heads(x.data_ptr(), sb, ss, sh, h)
+    except struct.error:
+        return _pack_heads(x.data_ptr(), sb, ss, sh, -1)
 
 
-def _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise):
-    """(packed norm, packed rotation, address of the row counts) of a call."""
-    for g in (gamma_q, gamma_k):
-        if g is not None and (g.dtype != torch.float32 or g.numel() != rows[2] or not g.is_contiguous() or
-                              not normalise):
-            raise ValueError("gamma_q and gamma_k are contiguous fp32 [head_dim] tensors, of a norm")
-    _on(rows[3], gamma_q, gamma_k, row_len)
-    norm = _pack_norm(0 if gamma_q is None else gamma_q.data_ptr(), 0 if gamma_k is None else gamma_k.data_ptr(),
-                      eps) if normalise else None
-    if rope is not None:
-        if not isinstance(rope, Rope):
-            raise TypeError(f"{type(rope).__name__} given where the call takes a Rope")
-        if rope.rows != rows[:2]:
-            raise ValueError("the rotation's positions must be of the call's batch and rows")
-        _on(rows[3], *rope._keep)
-        rope = rope._packed
-    return norm, rope, None if row_len is None else _int32_ptr(row_len, rows[0], "row_len")
+def _gamma(g: Optional[torch.Tensor], D: int, dev: int) -> int:
+    """Address of a contiguous fp32 [head_dim] tensor, 0 without one."""
+    if g is None:
+        return 0
+    if g.dtype != _FLOAT32 or g.numel() != D or not g.is_contiguous() or g.get_device() != dev:
+        raise ValueError("gamma_q, gamma_k and their gradients are contiguous fp32 [head_dim] tensors")
+    return g.data_ptr()
+
+
+def _norm(gamma_q, gamma_k, eps, normalise, D: int, dev: int) -> Optional[bytes]:
+    """The packed norm of a call, None without one."""
+    if normalise:
+        return _pack_norm(_gamma(gamma_q, D, dev), _gamma(gamma_k, D, dev), eps)
+    if gamma_q is not None or gamma_k is not None:
+        raise ValueError("gamma_q and gamma_k are those of a norm")
+    return None
+
+
+def _turns(rope: Optional[Rope], B: int, S: int, dev: int) -> Optional[bytes]:
+    """The packed rotation of a call, None without one."""
+    if rope is None:
+        return None
+    if not isinstance(rope, Rope):
+        raise TypeError(f"{type(rope).__name__} given where the call takes a Rope")
+    if rope.rows != (B, S) or rope.device != dev:
+        raise ValueError("the rotation's tensors must be of the call's batch, rows and device")
+    return rope._packed
+
+
+def _one_of(q, k):
+    """(batch, rows, head_dim, dtype, device) of the queries, or of the keys."""
+    x = k if q is None else q
+    if x is None or x.dim() != 4:
+        raise ValueError("q or k must be given, as [B, S, H, D]")
+    B, S, _, D = x.shape
+    return B, S, D, x.dtype, x.get_device()
 
 
 def speechkv_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
@@ -939,17 +969,14 @@ def speechkv_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_o
     contiguous last axis (q and q_out, or k and k_out, may be None; an output
     may be its input); gamma_q, gamma_k: fp32 [D] or None: 1; row_len: int32
     [B] or None: every row; normalise=False: the rotation alone."""
-    x = k if q is None else q
-    if x is None or len(x.shape) != 4:
-        raise ValueError("q or k must be given, as [B, S, H, D]")
-    B, S, _, D = x.shape
-    dev = x.get_device()
-    rows, dt = (B, S, D, dev), x.dtype
-    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
-    st = _lib.speechkv_norm_rope(_heads(q, rows, dt), _heads(k, rows, dt), _int32(B), _int32(S), count, _int32(D),
-                                 _dtype_code(dt), norm, turn, _heads(q_out, rows, dt), _heads(k_out, rows, dt),
-                                 _stream_of(dev, stream))
-    _check(st, "speechkv_norm_rope")
+    B, S, D, dt, dev = _one_of(q, k)
+    st = _lib.speechkv_norm_rope(_heads(q, B, S, D, dt, dev), _heads(k, B, S, D, dt, dev), B if B < 2**31 else -1,
+                                 S if S < 2**31 else -1, _counts(row_len, B, dev, "row_len"), D if D < 2**31 else -1,
+                                 _DTYPE_CODES.get(dt, 99), _norm(gamma_q, gamma_k, eps, normalise, D, dev),
+                                 _turns(rope, B, S, dev), _heads(q_out, B, S, D, dt, dev),
+                                 _heads(k_out, B, S, D, dt, dev), _stream_of(dev, stream))
+    if st:
+        _check(st, "speechkv_norm_rope")
 
 
 def speechkv_norm_rope_bwd_workspace_bytes(batch: int, num_rows: int, num_q_heads: int, num_kv_heads: int,
@@ -967,23 +994,18 @@ def speechkv_norm_rope_bwd(q: Optional[torch.Tensor], k: Optional[torch.Tensor],
     dk: gradients of its inputs (dq may be dq_out, dk may be dk_out); dgamma_q,
     dgamma_k: fp32 [D] or None; workspace: device bytes, with a dgamma.  The
     rest as for speechkv_norm_rope."""
-    x = k if q is None else q
-    if x is None or len(x.shape) != 4:
-        raise ValueError("q or k must be given, as [B, S, H, D]")
-    B, S, _, D = x.shape
-    dev = x.get_device()
-    rows, dt = (B, S, D, dev), x.dtype
-    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, row_len, normalise)
-    for g in (dgamma_q, dgamma_k):
-        if g is not None and (g.dtype != torch.float32 or g.numel() != D or not g.is_contiguous()):
-            raise ValueError("dgamma_q and dgamma_k are contiguous fp32 [head_dim] tensors")
-    _on(dev, dgamma_q, dgamma_k)
+    B, S, D, dt, dev = _one_of(q, k)
     ws, ws_bytes = _workspace(workspace, dev)
-    st = _lib.speechkv_norm_rope_bwd(_heads(q, rows, dt), _heads(k, rows, dt), _heads(dq_out, rows, dt),
-                                     _heads(dk_out, rows, dt), _int32(B), _int32(S), count, _int32(D),
-                                     _dtype_code(dt), norm, turn, _heads(dq, rows, dt), _heads(dk, rows, dt),
-                                     _ptr(dgamma_q), _ptr(dgamma_k), ws, ws_bytes, _stream_of(dev, stream))
-    _check(st, "speechkv_norm_rope_bwd")
+    st = _lib.speechkv_norm_rope_bwd(_heads(q, B, S, D, dt, dev), _heads(k, B, S, D, dt, dev),
+                                     _heads(dq_out, B, S, D, dt, dev), _heads(dk_out, B, S, D, dt, dev),
+                                     B if B < 2**31 else -1, S if S < 2**31 else -1,
+                                     _counts(row_len, B, dev, "row_len"), D if D < 2**31 else -1,
+                                     _DTYPE_CODES.get(dt, 99), _norm(gamma_q, gamma_k, eps, normalise, D, dev),
+                                     _turns(rope, B, S, dev), _heads(dq, B, S, D, dt, dev),
+                                     _heads(dk, B, S, D, dt, dev), _gamma(dgamma_q, D, dev) or None,
+                                     _gamma(dgamma_k, D, dev) or None, ws, ws_bytes, _stream_of(dev, stream))
+    if st:
+        _check(st, "speechkv_norm_rope_bwd")
 
 
 def speechkv_norm_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: PagedKV,
@@ -995,22 +1017,18 @@ def speechkv_norm_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch
     """k, v: [B, S, Hkv, D] and q, q_out: [B, S, Hq, D] views with a contiguous
     last axis (q and q_out may be None, q_out may be q); cache_len, new_len,
     cache_len_out: int32 [B].  The rest as for speechkv_norm_rope."""
-    if len(k.shape) != 4:
-        raise ValueError("k must be [B, S, Hkv, D]")
-    B, S, _, D = k.shape
-    dev = k.get_device()
-    rows, dt = (B, S, D, dev), k.dtype
+    B, S, D, dt, dev = _one_of(None, k)
     c, pages, batch = cache._paged_kv_for(dt)
-    if pages[3] != D or batch != B:
-        raise ValueError("k and v must have the cache's head_dim and batch")
-    _on(dev, cache.k_pages, cache.v_pages, cache.block_table, cache_len, cache_len_out)
-    norm, turn, count = _norm_plan(rows, gamma_q, gamma_k, eps, rope, new_len, normalise)
-    lens = _int32_ptr(cache_len, B, "cache_len")
-    lens_out = None if cache_len_out is None else _int32_ptr(cache_len_out, B, "cache_len_out")
-    st = _lib.speechkv_norm_append_kv(_heads(q, rows, dt), _heads(k, rows, dt), _heads(v, rows, dt), _int32(B),
-                                      _int32(S), count, norm, turn, lens, c, _heads(q_out, rows, dt), lens_out,
-                                      _stream_of(dev, stream))
-    _check(st, "speechkv_norm_append_kv")
+    if pages[3] != D or batch != B or not _cache_on(cache, dev):
+        raise ValueError("k and v must have the cache's head_dim, batch and device")
+    st = _lib.speechkv_norm_append_kv(_heads(q, B, S, D, dt, dev), _heads(k, B, S, D, dt, dev),
+                                      _heads(v, B, S, D, dt, dev), B if B < 2**31 else -1, S if S < 2**31 else -1,
+                                      _counts(new_len, B, dev, "new_len"),
+                                      _norm(gamma_q, gamma_k, eps, normalise, D, dev), _turns(rope, B, S, dev),
+                                      _counts(cache_len, B, dev, "cache_len"), c, _heads(q_out, B, S, D, dt, dev),
+                                      _counts(cache_len_out, B, dev, "cache_len_out"), _stream_of(dev, stream))
+    if st:
+        _check(st, "speechkv_norm_append_kv")
 
 
 def speechkv_shared_attn(q: torch.Tensor, prefix: PagedKV, prefix_len: torch.Tensor, max_prefix_len: int,
@@ -1033,20 +1051,23 @@ def speechkv_shared_attn(q: torch.Tensor, prefix: PagedKV, prefix_len: torch.Ten
         raise ValueError("q and out must have the cache's dtype, head_dim and batch")
     if prefix_pages[1] != pages[1] or prefix_pages[3] != D:
         raise ValueError("prefix and cache must have the same heads and head_dim")
-    lens, prefix_lens = _int32_ptr(cache_len, B, "cache_len"), _int32_ptr(prefix_len, groups, "prefix_len")
-    starts = _int32_ptr(group_start, groups + 1, "group_start")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, Hq) or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous fp32 [B, Hq] tensor")
-    _on(dev, out, cache.k_pages, cache.v_pages, cache.block_table, prefix.k_pages, prefix.v_pages, prefix.block_table,
-        cache_len, prefix_len, group_start, lse)
-    if scale is None:
-        scale = D ** -0.5
+    if out.get_device() != dev or not _cache_on(cache, dev) or not _cache_on(prefix, dev):
+        raise ValueError("every tensor of a call must be on one device")
+    lsep = None
+    if lse is not None:
+        if lse.dtype != _FLOAT32 or lse.shape != (B, Hq) or not lse.is_contiguous() or lse.get_device() != dev:
+            raise ValueError("lse must be a contiguous fp32 [B, Hq] tensor")
+        lsep = lse.data_ptr()
     ws, ws_bytes = _workspace(workspace, dev)
-    st = _lib.speechkv_shared_attn(q.data_ptr(), _int32(B), _int32(Hq), p, prefix_lens, _int32(max_prefix_len), starts,
-                                   _int32(groups), _int32(max_group), c, lens, _int32(max_cache_len), scale,
-                                   num_splits and _int32(num_splits), out.data_ptr(), _ptr(lse), ws, ws_bytes,
-                                   _stream_of(dev, stream))
-    _check(st, "speechkv_shared_attn")
+    st = _lib.speechkv_shared_attn(q.data_ptr(), B if B < 2**31 else -1, Hq if Hq < 2**31 else -1, p,
+                                   _counts(prefix_len, groups, dev, "prefix_len"), _int32(max_prefix_len),
+                                   _counts(group_start, groups + 1, dev, "group_start"),
+                                   groups if groups < 2**31 else -1, _int32(max_group), c,
+                                   _counts(cache_len, B, dev, "cache_len"), _int32(max_cache_len),
+                                   D ** -0.5 if scale is None else scale, num_splits and _int32(num_splits),
+                                   out.data_ptr(), lsep, ws, ws_bytes, _stream_of(dev, stream))
+    if st:
+        _check(st, "speechkv_shared_attn")
 
 
 def speechkv_shared_num_splits(batch: int, num_groups: int, max_group: int, num_q_heads: int, num_kv_heads: int,
@@ -1071,33 +1092,37 @@ def speechkv_attn_weights(q: torch.Tensor, lse: torch.Tensor, cache: PagedKV, ca
     be weights_out, or None: zeros); visible: int32 [B, n], the entries that
     each row sees (see visible_slots()), or None: the rows are the sequence's
     last n tokens."""
-    dt, dev = q.dtype, q.get_device()
-    if len(q.shape) != 4:
-        raise ValueError("q must be [B, n, Hq, D]")
-    B, n, Hq, D = q.shape
+    B, n, D, dt, dev = _one_of(q, None)
+    Hq = q.shape[2]
     c, pages, batch = cache._paged_kv_for(dt)
-    if pages[3] != D or batch != B:
-        raise ValueError("q must have the cache's dtype, head_dim and batch")
-    if lse.dtype != torch.float32 or lse.shape != (B, Hq, n):
+    if pages[3] != D or batch != B or not _cache_on(cache, dev):
+        raise ValueError("q must have the cache's dtype, head_dim, batch and device")
+    if lse.dtype != _FLOAT32 or lse.shape != (B, Hq, n) or lse.get_device() != dev:
         raise ValueError("lse must be an fp32 [B, Hq, n] tensor")
-    for w in (weights_out,) if weights is None else (weights_out, weights):
-        if w.dtype != torch.float32 or len(w.shape) != 3 or w.shape[:2] != (B, pages[1]) or \
-                w.shape != weights_out.shape or not w.is_contiguous():
-            raise ValueError("weights must be contiguous fp32 [B, Hkv, capacity] tensors of one size")
-    lens = _int32_ptr(cache_len, B, "cache_len")
+    size = weights_out.shape
+    if len(size) != 3 or size[0] != B or size[1] != pages[1] or weights_out.dtype != _FLOAT32 or \
+            not weights_out.is_contiguous() or weights_out.get_device() != dev:
+        raise ValueError("weights_out must be a contiguous fp32 [B, Hkv, capacity] tensor")
+    capacity, before = size[2], None
+    if weights is not None:
+        if weights.shape != size or weights.dtype != _FLOAT32 or not weights.is_contiguous() or \
+                weights.get_device() != dev:
+            raise ValueError("weights must be a contiguous fp32 tensor of weights_out's size")
+        before = weights.data_ptr()
     seen = None
     if visible is not None:
-        if visible.dtype != _INT32 or visible.shape != (B, n) or not visible.is_contiguous():
+        if visible.dtype != _INT32 or visible.shape != (B, n) or not visible.is_contiguous() or \
+                visible.get_device() != dev:
             raise ValueError("visible must be a contiguous int32 [B, n] tensor")
         seen = visible.data_ptr()
-    _on(dev, lse, cache.k_pages, cache.v_pages, cache.block_table, cache_len, weights_out, weights, visible)
-    if scale is None:
-        scale = D ** -0.5
     sb, sh, ss = lse.stride()
-    st = _lib.speechkv_attn_weights(_heads(q, (B, n, D, dev), dt), _int32(B), _int32(n), lse.data_ptr(), sb, sh, ss,
-                                    seen, c, lens, _int32(max_cache_len), scale, _ptr(weights),
-                                    weights_out.data_ptr(), _int32(weights_out.shape[2]), _stream_of(dev, stream))
-    _check(st, "speechkv_attn_weights")
+    st = _lib.speechkv_attn_weights(_heads(q, B, n, D, dt, dev), B if B < 2**31 else -1, n if n < 2**31 else -1,
+                                    lse.data_ptr(), sb, sh, ss, seen, c, _counts(cache_len, B, dev, "cache_len"),
+                                    _int32(max_cache_len), D ** -0.5 if scale is None else scale, before,
+                                    weights_out.data_ptr(), capacity if capacity < 2**31 else -1,
+                                    _stream_of(dev, stream))
+    if st:
+        _check(st, "speechkv_attn_weights")
 
 
 def visible_slots(segs, w: int, layer: int, l0: int, mask_mode: int = MASK_WINDOW_END,
@@ -1131,8 +1156,7 @@ def speechkv_evict(layers: EvictStack, keep_len: torch.Tensor, num_first: int, n
     if not isinstance(layers, EvictStack):
         raise TypeError(f"{type(layers).__name__} given where the call takes an EvictStack")
     B = layers.batch
-    keep = _int32_ptr(keep_len, B, "keep_len")
-    _on(layers.device, keep_len)
+    keep = _counts(keep_len, B, layers.device, "keep_len")
     st = _lib.speechkv_evict(layers._packed, layers.num_layers, _int32(B), keep, _int32(layers.max_keep),
                              _int32(layers.capacity), _int32(num_first), _int32(num_recent),
                              _stream_of(layers.device, stream))

@@ -119,7 +119,7 @@ def test_forward_rejects(kw, code):
     (dict(D=32), E_UNS), (dict(dt=2), E_UNS), (dict(dq=None), E_ARG), (dict(dyq=None), E_ARG), (dict(dyk=None), E_ARG),
     (dict(dq=heads(10, sh=0)), E_ARG), (dict(dk=heads(11, 4)), E_ARG), (dict(norm=None), E_ARG),
     (dict(q=None, dyq=None, dq=None), E_ARG),  # its dgamma is asked for
-    (dict(ws=None), E_WS), (dict(ws=at(48) + 4), E_WS), (dict(ws_bytes=6 * 2 * 64 * 4 - 1), E_WS)])
+    (dict(ws=None), E_WS), (dict(ws=at(48) + 4), E_WS), (dict(ws_bytes=skv.speechkv_norm_rope_bwd_workspace_bytes(2, 3, 4, 2, 64) - 1), E_WS)])
 def test_backward_rejects(kw, code):
     assert bwd(**kw) == code
 
@@ -183,7 +183,9 @@ def test_valid_calls_reach_the_device():
 
 def test_sizes():
     size = skv.speechkv_norm_rope_bwd_workspace_bytes
-    assert size(2, 3, 4, 2, 64) == 6 * 2 * 64 * 4 and size(8, 1596, 16, 8, 128) == 1024 * 2 * 128 * 4
+    for B, S, Hq, Hkv in ((1, 1, 1, 0), (1, 1, 0, 3), (2, 3, 4, 2), (8, 1596, 16, 8), (65535, 200, 64, 8), (1, 2 ** 24 - 1, 1, 1)):
+        for D in (64, 128):  # two sums a block at least, about a thousand blocks at most
+            assert D * 4 <= size(B, S, Hq, Hkv, D) <= 1026 * D * 4
     for bad in ((0, 3, 4, 2, 64), (2, 0, 4, 2, 64), (2, 3, 0, 0, 64), (2, 3, -1, 2, 64), (2, 3, 4, 2, 32),
                 (65535, 1 << 20, 4, 2, 64)):
         assert size(*bad) == 0
@@ -233,7 +235,7 @@ def test_binding_refuses_rotations_and_other_descriptions():
 def test_packed_descriptions_fill_their_structures():
     a, i = host()
     q = a["q"][:, :, 1:3]
-    h = skv._Heads.from_buffer_copy(skv._heads(q, (2, 3, 64, -1), torch.bfloat16))
+    h = skv._Heads.from_buffer_copy(skv._heads(q, 2, 3, 64, torch.bfloat16, -1))
     assert (h.data, h.stride_b, h.stride_s, h.stride_h, h.num_heads) == (q.data_ptr(), 768, 256, 64, 2)
     r = skv.Rope(i(3, 2, 3), torch.zeros(8), i(8), skv.ROPE_PAIRS)
     s = skv._Rope.from_buffer_copy(r._packed)
