@@ -23,7 +23,8 @@ namespace skv {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;                  // few rows
+constexpr int kManyWaves = 8, kManyThreads = 64 * kManyWaves;  // many rows
 constexpr int kSpreadUnits = 32;  // pairs from which an XCD takes pairs of its own
 
 // Rows of 16-byte chunks in LDS: chunk c of row r at position c ^ swizzle(r).
@@ -111,16 +112,15 @@ struct Unit {
 };
 __device__ __forceinline__ bool unit_of(const WeightArgs& a, Unit& u) {
   const int heads = a.cache.pv.kv_heads, pairs = a.batch * heads;
-  // An XCD (block index mod 8) takes neighbouring pairs: the KV heads of a
-  // sequence, whose rows lie beside each other.
+  // The first keys of all pairs, which most rows of a prompt see, come first.  An
+  // XCD (block index mod 8) takes neighbouring pairs: the KV heads of a sequence,
+  // whose rows lie beside each other.
   if (pairs >= kSpreadUnits) {
-    const int per = (pairs + 7) / 8;
-    a.by_key_blocks.divide((int)(blockIdx.x >> 3), u.pair, u.part);
-    if (u.pair >= per) return false;
-    u.pair += (int)(blockIdx.x & 7) * per;
+    a.by_pairs.divide((int)(blockIdx.x >> 3), u.part, u.pair);
+    u.pair += (int)(blockIdx.x & 7) * a.by_pairs.d;
     if (u.pair >= pairs) return false;
   } else {
-    a.by_key_blocks.divide((int)blockIdx.x, u.pair, u.part);
+    a.by_pairs.divide((int)blockIdx.x, u.part, u.pair);
   }
   a.by_heads.divide(u.pair, u.b, u.g);
   const PagedView& pv = a.cache.pv;
@@ -313,16 +313,15 @@ __global__ __launch_bounds__(kThreads, 2) void weights_few_kernel(WeightArgs a) 
 // --------------------------------------------------------------- many rows
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a) {
+__global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a) {
   typedef Rows16<T, D> L;
   constexpr int kKeys = weight_keys(L::kBytes), kTiles = kKeys / 16;
   constexpr int kAhead = L::kBytes > 256 ? 2 : 4;  // row tiles of a wave on their way
-  constexpr int kN = L::kTileLoads + 2;            // direct loads of a row tile
-  __shared__ __attribute__((aligned(1024))) unsigned char s_row[kWaves][kAhead][L::kTileBytes];
-  __shared__ float s_lse[kWaves][kAhead][64];
-  __shared__ int s_seen[kWaves][kAhead][64];
-  __shared__ float s_part[kWaves][kKeys];
-  __shared__ uint64_t s_sees[kWaves];
+  constexpr int kN = L::kTileLoads + 1;            // direct loads of a row tile
+  __shared__ __attribute__((aligned(1024))) unsigned char s_row[kManyWaves][kAhead][L::kTileBytes];
+  __shared__ int s_info[kManyWaves][kAhead][64];  // lanes 0 .. 31: the rows' lse, 32 .. 63: what they see
+  __shared__ float s_part[kManyWaves][kKeys];
+  __shared__ uint64_t s_sees[kManyWaves];
   static_assert(sizeof(s_row) >= kTiles * L::kTileBytes, "the keys come through the rows' place");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quarter = lane >> 4;
@@ -331,6 +330,29 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
   const int kb = u.part * kKeys;
   if (kb >= u.len) return;
 
+  float sum[4 * kTiles];
+#pragma unroll
+  for (int j = 0; j < 4 * kTiles; ++j) sum[j] = 0.f;
+  const int queries = 16 >> a.group_shift, in = col >> a.group_shift;
+
+  // kManyWaves * 64 row tiles at a time, 64 a wave: lane n finds out whether any row
+  // of tile n sees these keys.  Every wave then goes through those tiles of its own
+  // (one in kManyWaves) that do, kAhead of them requested ahead.  From the last row to
+  // the first: in a prompt the last rows see most, so the blocks of a sequence read
+  // the same rows at the same time, out of one L2.
+  auto scan = [&](int rt0) {
+    int most = 0;
+#pragma unroll 8
+    for (int n = 0; n < queries; ++n) {
+      const int i = (rt0 + 64 * wave + lane) * queries + n;
+      most = max(most, seen_of(a, u, *seen_at(a, u, i), i));
+    }
+    return __builtin_amdgcn_ballot_w64(most > kb);
+  };
+  int rt0 = (a.row_tiles - 1) / (64 * kManyWaves) * (64 * kManyWaves);
+  const int rt0_first = rt0;
+  uint64_t sees;
+
   u32x4_t k[kTiles][L::kPieces];
   uint64_t present;  // keys that have a page
   {
@@ -338,7 +360,8 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
     const int entry = table[min(kb + lane, u.len - 1) >> a.cache.pv.page_shift];
     present = __builtin_amdgcn_ballot_w64(entry >= 0 && entry < a.cache.pv.num_pages);
     const uint32_t sk = lds_addr(s_row);
-    load_keys<T, D, kTiles, 0, false>(a, u, kb, entry, 0, sk, lane, wave, kWaves);
+    load_keys<T, D, kTiles, 0, false>(a, u, kb, entry, 0, sk, lane, wave, kManyWaves);
+    sees = scan(rt0);  // (on its way with the keys)
     wait_vm<0>();
     __syncthreads();
 #pragma unroll
@@ -347,38 +370,39 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
     __syncthreads();  // the keys are in registers: rows take their place
   }
 
-  float sum[4 * kTiles];
+  const uint32_t s_rows = lds_addr(s_row[wave]), s_infos = lds_addr(s_info[wave]);
+  // where this lane reads its share of a tile: in a tile whose queries are all there,
+  // as far behind tile 0's as the tile's first query behind query 0
+  const char* from[L::kTileLoads];
 #pragma unroll
-  for (int j = 0; j < 4 * kTiles; ++j) sum[j] = 0.f;
-  const int queries = 16 >> a.group_shift, in = col >> a.group_shift;
-  const uint32_t s_rows = lds_addr(s_row[wave]), s_lses = lds_addr(s_lse[wave]), s_seens = lds_addr(s_seen[wave]);
+  for (int n = 0; n < L::kTileLoads; ++n) {
+    const int row = n * L::kPerLoad + lane / L::kChunks;
+    from[n] = row_of<T>(a, u, 0, row) + ((lane % L::kChunks ^ L::swizzle(row)) << 4);
+  }
+  const int64_t row_step = queries * a.q.ss * (int)sizeof(T);
   auto request = [&](int rt, int buffer) __attribute__((always_inline)) {
-    load_rows<T, D>(a, u, rt, s_rows + buffer * L::kTileBytes, lane);
-    lds_dma4(lse_of(a, u, rt, col), __builtin_amdgcn_readfirstlane(s_lses + buffer * 256));
-    lds_dma4(seen_at(a, u, rt * queries + in), __builtin_amdgcn_readfirstlane(s_seens + buffer * 256));
+    if ((rt + 1) * queries <= a.num_rows) {
+#pragma unroll
+      for (int n = 0; n < L::kTileLoads; ++n)
+        lds_dma16_from<false>(from[n] + rt * row_step,
+                              __builtin_amdgcn_readfirstlane(s_rows + buffer * L::kTileBytes + n * 1024));
+    } else {
+      load_rows<T, D>(a, u, rt, s_rows + buffer * L::kTileBytes, lane);
+    }
+    lds_dma4(lane < 32 ? static_cast<const void*>(lse_of(a, u, rt, col)) : seen_at(a, u, rt * queries + in),
+             __builtin_amdgcn_readfirstlane(s_infos + buffer * 256));
   };
 
-  // kWaves * 64 row tiles at a time, 64 a wave: lane n finds out whether any row of
-  // tile n sees these keys.  Every wave then goes through those tiles of its own (one
-  // in kWaves) that do, kAhead of them requested ahead.  From the last row to the
-  // first: in a prompt the last rows see most, so the blocks of a sequence read the
-  // same rows at the same time, out of one L2.
-  constexpr uint64_t kMine = 0x1111111111111111ull;
-  static_assert(kWaves == 4, "tiles of a wave");
-  for (int rt0 = (a.row_tiles - 1) / (64 * kWaves) * (64 * kWaves); rt0 >= 0; rt0 -= 64 * kWaves) {
-    int most = 0;
-#pragma unroll 8
-    for (int n = 0; n < queries; ++n) {
-      const int i = (rt0 + 64 * wave + lane) * queries + n;
-      most = max(most, seen_of(a, u, *seen_at(a, u, i), i));
-    }
-    const uint64_t sees = __builtin_amdgcn_ballot_w64(most > kb);
+  static_assert(kManyWaves == 8, "tiles of a wave");
+  const uint64_t mine = 0x0101010101010101ull << wave;  // bits of the tiles that are this wave's
+  for (bool more = true; more; more = (rt0 -= 64 * kManyWaves) >= 0) {
+    if (rt0 != rt0_first) sees = scan(rt0);
     __syncthreads();  // (the last masks have been read)
     if (lane == 0) s_sees[wave] = sees;
     __syncthreads();
-    int count = 0, word = kWaves;
+    int count = 0, word = kManyWaves;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) count += __builtin_popcountll(s_sees[w] & (kMine << wave));
+    for (int w = 0; w < kManyWaves; ++w) count += __builtin_popcountll(s_sees[w] & mine);
     count = __builtin_amdgcn_readfirstlane(count);
     if (!count) continue;
     uint64_t todo = 0;
@@ -386,7 +410,7 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
     auto next = [&]() {  // the wave's next tile, the last one again behind it
       while (!todo && word > 0) {
         --word;
-        const uint64_t x = s_sees[word] & (kMine << wave);
+        const uint64_t x = s_sees[word] & mine;
         todo = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 |
                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x);
       }
@@ -406,8 +430,8 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
         wait_vm<(kAhead - 1) * kN>();
         u32x4_t x[L::kPieces];
         L::read(x, s_rows + j * L::kTileBytes, col, quarter);
-        const float l = s_lse[wave][j][lane];
-        const int seen = seen_of(a, u, s_seen[wave][j][lane], tile[j] * queries + in);
+        const float l = __int_as_float(s_info[wave][j][col]);
+        const int seen = seen_of(a, u, s_info[wave][j][32 + col], tile[j] * queries + in);
         wait_lds();
         request(tile[j] = next(), j);  // (always: what waits for the others counts on it)
         if (at + j < count) add_rows<T, D, kTiles>(a, k, x, l, seen, kb, quarter, sum);
@@ -420,7 +444,7 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
   if (tid < kKeys && kb + tid < u.len) {
     float total = 0.f;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) total += s_part[v][tid];
+    for (int v = 0; v < kManyWaves; ++v) total += s_part[v][tid];
     const int64_t to = (int64_t)u.pair * a.capacity + kb + tid;
     a.weights_out[to] = (a.weights ? a.weights[to] : 0.f) + (present >> tid & 1 ? total : 0.f);
   }
@@ -431,12 +455,13 @@ __global__ __launch_bounds__(kThreads, 2) void weights_many_kernel(WeightArgs a)
 template <typename T, int D>
 hipError_t launch_weights_d(const WeightArgs& args, hipStream_t s) {
   WeightArgs a = args;
-  a.by_key_blocks = FastDivide(a.key_blocks);
   a.by_heads = FastDivide(a.cache.pv.kv_heads);
   const int64_t pairs = (int64_t)a.batch * a.cache.pv.kv_heads;
-  const dim3 grid((uint32_t)((pairs >= kSpreadUnits ? (pairs + 7) / 8 * 8 : pairs) * a.key_blocks)), block(kThreads);
-  return a.row_tiles > kWeightFew ? launch_struct(weights_many_kernel<T, D>, grid, block, s, a)
-                                  : launch_struct(weights_few_kernel<T, D>, grid, block, s, a);
+  const bool spread = pairs >= kSpreadUnits;
+  a.by_pairs = FastDivide((int32_t)(spread ? (pairs + 7) / 8 : pairs));  // (of an XCD)
+  const dim3 grid((uint32_t)((spread ? (pairs + 7) / 8 * 8 : pairs) * a.key_blocks));
+  return a.row_tiles > kWeightFew ? launch_struct(weights_many_kernel<T, D>, grid, dim3(kManyThreads), s, a)
+                                  : launch_struct(weights_few_kernel<T, D>, grid, dim3(kThreads), s, a);
 }
 
 hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStream_t s) {

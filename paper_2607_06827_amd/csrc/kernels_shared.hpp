@@ -51,7 +51,7 @@ struct WeightArgs {
   int row_tiles;   // tiles of 16 rows of a (sequence, KV head)
   int steps;       // with few rows: steps of a wave (set by the plan, as key_blocks)
   int key_blocks;  // blocks of a (sequence, KV head)
-  FastDivide by_key_blocks, by_heads;  // (set by the launcher)
+  FastDivide by_pairs, by_heads;  // (set by the launcher)
 };
 constexpr int kWeightFew = 2;     // row tiles that a block keeps in LDS
 constexpr int kWeightStep = 32;   // keys of a wave's step with few rows
