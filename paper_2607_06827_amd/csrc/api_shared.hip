@@ -29,15 +29,55 @@ size_t shared_bytes(int32_t batch, int32_t q_heads, int32_t head_dim, const Shar
   return (size_t)batch * q_heads * (p.splits + p.own_splits) * (head_dim + 2) * sizeof(float);
 }
 
+// The plan with the smallest estimated time (with the given prefix splits, or of its
+// own choice).
+// The estimate is fitted to a sweep on MI355X over 20 shapes of 1 to 64 sequences
+// in 1 to 20 groups, 1 to 8 KV heads of 1 to 8 query heads, prefixes of 126 to 7532
+// and own caches of 10 to 5000 entries, both element types and head sizes; its
+// choice takes 1.3% longer than the best of the candidates on average, 11% at most.
+// In us:
+//  - a block takes 2, a step of a block's waves over a 128-wide bf16 tile 1.23, 1.11
+//    or 0.88 with 1, 2 or 4 row groups, one of a wave with own entries 1.27; 64-wide
+//    heads take 0.62 of it, fp32 5.1 and 2.5 times; what runs at once is two blocks a
+//    CU (four with 64-wide bf16 heads, one with 128-wide fp32);
+//  - a key is read at 6.5 TB/s, and again by every further row tile at 0.65 of the
+//    cost;
+//  - each partial row is written and read at 3.3 TB/s.
 SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_heads, int head_dim, int dtype,
                        int max_prefix, int max_len, int splits) {
-  const int64_t rows = (int64_t)max_group * group, tiles = tiles_of(max_prefix), own = tiles_of(max_len);
-  SharedPlan p;
-  p.groups = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  const int64_t units = (int64_t)groups * kv_heads * row_tiles_of(rows, p.groups);
-  p.splits = splits ? splits : (int)std::max<int64_t>(1, std::min<int64_t>({512 / units, (tiles + 3) / 4, 64}));
-  p.own_splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / ((int64_t)batch * kv_heads), (own + 7) / 8, 32}));
-  return p;
+  const bool f32 = dtype == SPEECHKV_DTYPE_F32, wide = head_dim == 128;
+  // members of a group: between the average and the bound
+  const double members = 0.5 * (max_group + std::min<double>(max_group, (double)batch / groups));
+  const double units = (double)groups * kv_heads, own_units = (double)batch * kv_heads, row_bytes = head_dim * (f32 ? 4.0 : 2.0);
+  const int64_t tiles = std::max<int64_t>(1, tiles_of(max_prefix)), own = std::max<int64_t>(1, tiles_of(max_len));
+  const double slots = 256.0 * (f32 && wide ? 1 : !f32 && !wide ? 4 : 2);
+  const double size = f32 ? (wide ? 5.07 : 2.45) : wide ? 1.0 : 0.62;
+  static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  SharedPlan best = {1, splits ? splits : 1, 1};
+  double best_us = 1e300;
+  for (int g = 1; g <= 4 && (g == 1 || max_group * (double)group > 16 * g); g *= 2) {
+    const double step_us = (g == 1 ? 1.23 : g == 2 ? 1.11 : 0.88) * size;
+    const double row_tiles = std::ceil(members * group / (32.0 * g));
+    for (int count : counts) {
+      const int s = splits ? splits : count;
+      if (!splits && s > tiles) break;
+      const double block_us = 1.98 + step_us * (double)(((tiles + s - 1) / s * g + 3) / 4);
+      for (int o : counts) {
+        if (o > own || o > 32) break;
+        const double own_us = 1.98 + 1.27 * size * (double)((own + o - 1) / o);
+        const double all_us = 1.12 * (units * row_tiles * s * block_us + std::ceil(own_units * o / 4) * own_us) / slots;
+        const double read_us = (units * max_prefix * (1 + 0.65 * (row_tiles - 1)) + own_units * max_len) * 2 * row_bytes / 6.5e6;
+        const double us = std::max({block_us, own_us, all_us, 1.98 + read_us}) + 0.2 * all_us +
+                          own_units * group * (s + o) * head_dim * 8 / 3.27e6;
+        if (us < best_us) {
+          best_us = us;
+          best = {g, s, o};
+        }
+      }
+      if (splits) break;
+    }
+  }
+  return best;
 }
 
 bool shared_sizes_bad(int32_t batch, int32_t num_groups, int32_t max_group, int32_t max_prefix_len,

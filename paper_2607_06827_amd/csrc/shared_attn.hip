@@ -5,8 +5,8 @@
 // G query heads of its group, are one matrix and the prefix is read once for all
 // of them; what they have of their own is read once each, with G rows.  Both are
 // partial results of the same softmax: blocks of one launch compute them (prefix
-// blocks: a group, KV head, range of its keys and up to 128 rows; own blocks: a
-// sequence, KV head and range of its keys), and a second launch merges a row's
+// blocks: a group, KV head, range of its keys and up to 128 rows; the waves of own
+// blocks: a sequence, KV head and range of its keys each), and a second launch merges a row's
 // partials by log-sum-exp, in a fixed order.
 //
 // A block of four waves takes 32, 64 or 128 rows (kGroups = 1, 2 or 4 row groups of
@@ -47,17 +47,19 @@ struct Job {
   int part;            // which partial result it is
 };
 
-// kOnce: no other block reads its keys.
-template <typename T, int D, int kGroups, bool kOnce>
+// kOnce: no other block reads its keys.  kAlone: every wave has a job of its own,
+// of at most 32 rows (kGroups = 1), and meets no barrier.
+template <typename T, int D, int kGroups, bool kOnce, bool kAlone>
 __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsigned char* s_tile, float (*s_m)[32],
                                        float (*s_l)[32]) {
   typedef Tile<T, D> L;
-  constexpr int kStreams = kWaves / kGroups;
+  static_assert(!kAlone || kGroups == 1, "a wave's rows");
+  constexpr int kStreams = kAlone ? 1 : kWaves / kGroups;
   constexpr int kShare = kKeys / kGroups, kRuns = kShare / 8;  // rows, runs of 8 rows that a wave loads
   constexpr int kLoadsPerWave = L::kLoads / kGroups, kVm = 2 * kLoadsPerWave;
   static_assert(L::kLoads % kGroups == 0 && kVm < 63, "vector-memory counter");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rg = wave % kGroups, stream = wave / kGroups;
+  const int rg = wave % kGroups, stream = kAlone ? 0 : wave / kGroups;
   const int col = lane & 31, hg = lane >> 5;
   const int parts = a.prefix_splits + a.own_splits, gshift = a.group_shift, gmask = (1 << gshift) - 1;
   const KeySource& src = *job.src;
@@ -69,7 +71,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
   };
   const int t_end = min(job.tile1, (job.keys + kKeys - 1) / kKeys), last = job.keys - 1;
   if (job.tile0 >= t_end) {  // nothing here: the merge passes over it
-    for (int r = job.row0 + tid; r < min(job.rows, job.row0 + 32 * kGroups); r += kWaves * 64) {
+    for (int r = job.row0 + (kAlone ? lane : tid); r < min(job.rows, job.row0 + 32 * kGroups); r += kWaves * 64) {
       const int64_t at = out_row(r) * parts + job.part;
       a.ws_ml[2 * at] = neg_inf();
       a.ws_ml[2 * at + 1] = 0.f;
@@ -302,7 +304,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
       }
     }
   }
-  __syncthreads();  // every wave is done with the tiles, and no load is in flight
+  if constexpr (!kAlone) __syncthreads();  // every wave is done with the tiles, and no load is in flight
 
   const float l_tot = partner_sum(l_run);
   if constexpr (kStreams == 1) {
@@ -373,11 +375,11 @@ __device__ __forceinline__ int keys_of(const KeySource& src, int entry) {
 }
 
 template <typename T, int D, int kGroups, bool kOnce>
-__global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1)) void shared_kernel(SharedArgs a) {
+__global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 || D == 64 ? 2 : 1)) void shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char s_tile[kWaves * 2 * Tile<T, D>::kBytes];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   static_assert(sizeof(s_tile) >= (kGroups == 1 ? 1 : 2) * (kWaves / kGroups) * 2 * Tile<T, D>::kBytes &&
-                    sizeof(s_tile) >= kWaves * 32 * D * (kGroups == 4 ? 0 : 4),
+                    sizeof(s_tile) >= kWaves * 32 * D * (kGroups == kWaves ? 0 : 4),
                 "two buffers a stream, or one a wave; the streams' sums");
   Job job;
   if ((int)blockIdx.x < a.prefix_blocks) {
@@ -396,11 +398,14 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1)) void shared_
     job.tile0 = split * a.prefix_tiles;
     job.tile1 = job.tile0 + a.prefix_tiles;
     job.part = split;
-    attend<T, D, kGroups, kOnce>(a, job, s_tile, s_m, s_l);
+    attend<T, D, kGroups, kOnce, false>(a, job, s_tile, s_m, s_l);
   } else {
+    // a (sequence, KV head) and split a wave
     int pair, split, b;
-    a.by_own_splits.divide((int)blockIdx.x - a.prefix_blocks, pair, split);
+    const int unit = ((int)blockIdx.x - a.prefix_blocks) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    a.by_own_splits.divide(unit, pair, split);
     a.by_heads.divide(pair, b, job.g);
+    if (b >= a.batch) return;
     job.src = &a.own;
     job.entry = job.first_b = b;
     job.rows = 1 << a.group_shift;
@@ -409,7 +414,7 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 ? 2 : 1)) void shared_
     job.tile0 = split * a.own_tiles;
     job.tile1 = job.tile0 + a.own_tiles;
     job.part = a.prefix_splits + split;
-    attend<T, D, 1, true>(a, job, s_tile, s_m, s_l);
+    attend<T, D, 1, true, true>(a, job, s_tile, s_m, s_l);
   }
 }
 
@@ -492,16 +497,16 @@ hipError_t launch_shared_d(const SharedArgs& args, hipStream_t s) {
   a.by_own_splits = FastDivide(a.own_splits);
   a.by_heads = FastDivide(heads);
   a.prefix_blocks = a.groups * heads * a.prefix_splits * a.row_tiles;
-  const dim3 grid((uint32_t)(a.prefix_blocks + (int64_t)a.batch * heads * a.own_splits)), block(kWaves * 64);
-  const bool once = a.row_tiles == 1;
-  if (a.row_groups == 1)
-    return once ? launch_struct(shared_kernel<T, D, 1, true>, grid, block, s, a)
-                : launch_struct(shared_kernel<T, D, 1, false>, grid, block, s, a);
-  if (a.row_groups == 2)
-    return once ? launch_struct(shared_kernel<T, D, 2, true>, grid, block, s, a)
-                : launch_struct(shared_kernel<T, D, 2, false>, grid, block, s, a);
-  return once ? launch_struct(shared_kernel<T, D, 4, true>, grid, block, s, a)
-              : launch_struct(shared_kernel<T, D, 4, false>, grid, block, s, a);
+  const int64_t own_units = (int64_t)a.batch * heads * a.own_splits;
+  const dim3 grid((uint32_t)(a.prefix_blocks + (own_units + kWaves - 1) / kWaves)), block(kWaves * 64);
+  auto launch = [&](auto groups) {
+    constexpr int G = decltype(groups)::value;
+    return a.row_tiles == 1 ? launch_struct(shared_kernel<T, D, G, true>, grid, block, s, a)
+                            : launch_struct(shared_kernel<T, D, G, false>, grid, block, s, a);
+  };
+  if (a.row_groups == 1) return launch(std::integral_constant<int, 1>());
+  if (a.row_groups == 2) return launch(std::integral_constant<int, 2>());
+  return launch(std::integral_constant<int, 4>());
 }
 
 hipError_t launch_shared(const SharedArgs& a, int dtype, int head_dim, hipStream_t s) {
