@@ -21,7 +21,9 @@ namespace skv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeld = 8;  // pieces a thread of the move holds
+constexpr int kFusedRows = 512;  // (layer, sequence, KV head)s from which one kernel does both
+constexpr int kHeld = 8;     // pieces a thread of the move holds
+constexpr int kKeysHeld = 8;  // weights a thread of the choice holds
 
 // Whole numbers in the order of the weights: 0 and -0 alike, NaN below all.
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -43,15 +45,18 @@ __device__ __forceinline__ Counts counts_of(const EvictArgs& a, const EvictLayer
   return c;
 }
 
-template <int kBlock>
-__global__ __launch_bounds__(kBlock) void evict_choose_kernel(EvictArgs a) {
-  constexpr int kWaves = kBlock / 64;
-  __shared__ uint32_t s_count[256];
-  __shared__ int s_digit, s_left;
-  __shared__ int s_stay[2][kWaves], s_equal[2][kWaves];
-  const EvictLayer& y = a.layer[blockIdx.z];
-  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Counts n = counts_of(a, y, b);
+struct ChoiceSpace {
+  uint32_t count[256];
+  int digit, left;
+  int stay[2][kThreads / 64], equal[2][kThreads / 64];
+};
+
+// The entries of head g of sequence b that stay, into kept and weights_out, by one
+// block.
+__device__ __forceinline__ void choose(const EvictArgs& a, const EvictLayer& y, int b, int g, const Counts& n,
+                                       ChoiceSpace& s) {
+  constexpr int kBlock = kThreads, kWaves = kThreads / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (g == 0 && tid == 0 && y.cache_len_out) y.cache_len_out[b] = n.keep;
   const int64_t row = (int64_t)b * a.kv_heads + g;
   const float* w = y.weights + row * a.capacity;
@@ -67,22 +72,38 @@ __global__ __launch_bounds__(kBlock) void evict_choose_kernel(EvictArgs a) {
   const int lo = n.first, hi = n.len - n.recent;  // the entries between
   const int m = n.keep - n.first - n.recent;      // of which so many stay
   // the m-th largest: digits from the top, among those that share the ones before
-  uint32_t least = 0;
+  // (a short row stays in registers between the passes)
+  uint32_t least = 0, held[kKeysHeld];
+  const bool is_held = hi - lo <= kKeysHeld * kBlock;
   int left = m;
   if (m > 0) {
+    if (is_held) {
+#pragma unroll
+      for (int t = 0; t < kKeysHeld; ++t) {
+        const int c = lo + tid + t * kBlock;
+        held[t] = c < hi ? order_of(w[c]) : 0u;
+      }
+    }
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kBlock) s_count[i] = 0;
+      s.count[tid] = 0;
+      static_assert(kBlock == 256, "a thread a digit");
       __syncthreads();
-      for (int c = lo + tid; c < hi; c += kBlock) {
-        const uint32_t x = order_of(w[c]);
-        if (shift == 24 || (x >> (shift + 8)) == (least >> (shift + 8))) atomicAdd(&s_count[x >> shift & 255u], 1u);
+      auto count = [&](uint32_t x) {
+        if (shift == 24 || (x >> (shift + 8)) == (least >> (shift + 8))) atomicAdd(&s.count[x >> shift & 255u], 1u);
+      };
+      if (is_held) {
+#pragma unroll
+        for (int t = 0; t < kKeysHeld; ++t)
+          if (lo + tid + t * kBlock < hi) count(held[t]);
+      } else {
+        for (int c = lo + tid; c < hi; c += kBlock) count(order_of(w[c]));
       }
       __syncthreads();
       if (wave == 0) {
         // lane i has the digits 4 i .. 4 i + 3; entries of digits above them
         int mine[4], sum = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum += mine[k] = (int)s_count[4 * lane + k];
+        for (int k = 0; k < 4; ++k) sum += mine[k] = (int)s.count[4 * lane + k];
         int above = sum;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -93,15 +114,15 @@ __global__ __launch_bounds__(kBlock) void evict_choose_kernel(EvictArgs a) {
 #pragma unroll
         for (int k = 3; k >= 0; --k) {
           if (above < left && left <= above + mine[k]) {
-            s_digit = 4 * lane + k;
-            s_left = left - above;
+            s.digit = 4 * lane + k;
+            s.left = left - above;
           }
           above += mine[k];
         }
       }
       __syncthreads();
-      least |= (uint32_t)s_digit << shift;
-      left = s_left;
+      least |= (uint32_t)s.digit << shift;
+      left = s.left;
     }
   }
   // `left` of those equal to `least` stay, the lowest slots first
@@ -114,21 +135,21 @@ __global__ __launch_bounds__(kBlock) void evict_choose_kernel(EvictArgs a) {
     const bool equal = between && m > 0 && key == least;
     const uint64_t eq = __builtin_amdgcn_ballot_w64(equal);
     const uint64_t before = ((uint64_t)1 << lane) - 1;
-    if (lane == 0) s_equal[turn][wave] = __popcll(eq);
+    if (lane == 0) s.equal[turn][wave] = __popcll(eq);
     __syncthreads();
     int rank = equals + __popcll(eq & before);
     for (int v = 0; v < kWaves; ++v) {
-      const int k = s_equal[turn][v];
+      const int k = s.equal[turn][v];
       if (v < wave) rank += k;
       equals += k;
     }
     const bool stay = c < n.len && (between ? m > 0 && (key > least || (equal && rank < left)) : true);
     const uint64_t st = __builtin_amdgcn_ballot_w64(stay);
-    if (lane == 0) s_stay[turn][wave] = __popcll(st);
+    if (lane == 0) s.stay[turn][wave] = __popcll(st);
     __syncthreads();  // (every weight of this stretch has been read)
     int to = stayed + __popcll(st & before);
     for (int v = 0; v < kWaves; ++v) {
-      const int k = s_stay[turn][v];
+      const int k = s.stay[turn][v];
       if (v < wave) to += k;
       stayed += k;
     }
@@ -141,20 +162,20 @@ __global__ __launch_bounds__(kBlock) void evict_choose_kernel(EvictArgs a) {
   for (int c = n.keep + tid; c < n.len; c += kBlock) out[c] = 0.f;
 }
 
-// kChunks: 16-byte pieces of a row.
+constexpr int kMost = kThreads * kHeld / 4;  // most entries of a stretch (a part has 4 pieces at least)
+struct MoveSpace {
+  int64_t from[kMost], to[kMost];  // rows in a pool, -1: not moved
+};
+
+// The rows of head g of sequence b in pool number v (0: keys, 1: values) move, by one
+// block: pieces part * cols .. of the kChunks 16-byte pieces of a row.
 template <int kChunks>
-__global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
-  constexpr int kMost = kThreads * kHeld / 4;  // entries of a stretch (a part has 4 pieces at least)
-  __shared__ int64_t s_from[kMost], s_to[kMost];  // rows in a pool, -1: not moved
-  const EvictLayer& y = a.layer[blockIdx.z];
-  const int b = blockIdx.y, tid = threadIdx.x;
-  const Counts n = counts_of(a, y, b);
-  if (n.keep == n.len) return;
-  const int part = blockIdx.x % a.parts, hv = blockIdx.x / a.parts, g = hv >> 1;
-  const int cols = kChunks / a.parts, stretch = kThreads * kHeld / cols;
+__device__ __forceinline__ void move(const EvictArgs& a, const EvictLayer& y, int b, int g, int v, int part, int cols,
+                                     const Counts& n, MoveSpace& s) {
+  const int tid = threadIdx.x, stretch = kThreads * kHeld / cols;
   const int32_t* kept = y.kept + ((int64_t)b * a.kv_heads + g) * a.max_keep;
   const int32_t* table = y.table + (int64_t)b * y.max_pages;
-  u32x4_t* pool = static_cast<u32x4_t*>(hv & 1 ? y.v_pages : y.k_pages) + part * cols;
+  u32x4_t* pool = static_cast<u32x4_t*>(v ? y.v_pages : y.k_pages) + part * cols;
   auto row_of = [&](int slot) -> int64_t {
     const int page = table[slot >> y.page_shift];  // (a slot below n.len is inside the table)
     if (page < 0 || page >= y.num_pages) return -1;
@@ -169,24 +190,70 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
         from = row_of(slot);
         to = row_of(first + j);
       }
-      s_from[j] = from;
-      s_to[j] = from < 0 ? -1 : to;
+      s.from[j] = from;
+      s.to[j] = from < 0 ? -1 : to;
     }
     __syncthreads();
     u32x4_t held[kHeld];
 #pragma unroll
     for (int t = 0; t < kHeld; ++t) {
       const int item = tid + t * kThreads, j = item / cols;
-      if (j < some && s_to[j] >= 0) held[t] = pool[s_from[j] * kChunks + (item & (cols - 1))];
+      if (j < some && s.to[j] >= 0)
+        held[t] = __builtin_nontemporal_load(pool + s.from[j] * kChunks + (item & (cols - 1)));
     }
-    __syncthreads();
+    __syncthreads();  // (every row of the stretch has been read)
 #pragma unroll
     for (int t = 0; t < kHeld; ++t) {
       const int item = tid + t * kThreads, j = item / cols;
-      if (j < some && s_to[j] >= 0) pool[s_to[j] * kChunks + (item & (cols - 1))] = held[t];
+      if (j < some && s.to[j] >= 0)
+        __builtin_nontemporal_store(held[t], pool + s.to[j] * kChunks + (item & (cols - 1)));
     }
     __syncthreads();  // (the lists have been read)
   }
+}
+
+// Few rows: the choice, then the moves as blocks of their own.
+__global__ __launch_bounds__(kThreads) void evict_choose_kernel(EvictArgs a) {
+  __shared__ ChoiceSpace s;
+  const EvictLayer& y = a.layer[blockIdx.z];
+  choose(a, y, blockIdx.y, blockIdx.x, counts_of(a, y, blockIdx.y), s);
+}
+
+template <int kChunks>
+__global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
+  __shared__ MoveSpace s;
+  const EvictLayer& y = a.layer[blockIdx.z];
+  const Counts n = counts_of(a, y, blockIdx.y);
+  if (n.keep == n.len) return;
+  const int part = blockIdx.x % a.parts, hv = blockIdx.x / a.parts;
+  move<kChunks>(a, y, blockIdx.y, hv >> 1, hv & 1, part, kChunks / a.parts, n, s);
+}
+
+// Many rows: a block chooses and moves, so that one block's choice runs beside
+// another's moves.
+template <int kChunks>
+__global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
+  __shared__ union {
+    ChoiceSpace choice;
+    MoveSpace moves;
+  } s;
+  const EvictLayer& y = a.layer[blockIdx.z];
+  const int b = blockIdx.y, g = blockIdx.x;
+  const Counts n = counts_of(a, y, b);
+  choose(a, y, b, g, n, s.choice);
+  if (n.keep == n.len) return;
+  __syncthreads();  // (the list is complete)
+  for (int v = 0; v < 2; ++v) move<kChunks>(a, y, b, g, v, 0, kChunks, n, s.moves);
+}
+
+template <int kChunks>
+hipError_t launch_evict_d(const EvictArgs& a, int layers, int batch, hipStream_t s) {
+  const dim3 rows(a.kv_heads, batch, layers), block(kThreads);
+  // ROWS rule
+  if ((int64_t)a.kv_heads * batch * layers >= kFusedRows) return launch_struct(evict_kernel<kChunks>, rows, block, s, a);
+  const hipError_t e = launch_struct(evict_choose_kernel, rows, block, s, a);
+  if (e != hipSuccess) return e;
+  return launch_struct(evict_move_kernel<kChunks>, dim3(2 * a.kv_heads * a.parts, batch, layers), block, s, a);
 }
 
 }  // namespace
@@ -194,14 +261,10 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(EvictArgs a) {
 hipError_t launch_evict(const EvictArgs& args, int dtype, int head_dim, int layers, int batch, hipStream_t s) {
   EvictArgs a = args;
   const int chunks = head_dim * (dtype == 1 ? 2 : 4) / 16;
-  a.parts = 1;
-  const dim3 rows(a.kv_heads, batch, layers);
-  hipError_t e = launch_struct(evict_choose_kernel<256>, rows, dim3(256), s, a);
-  if (e != hipSuccess) return e;
-  const dim3 grid(2 * a.kv_heads * a.parts, batch, layers), block(kThreads);
-  if (chunks == 8) return launch_struct(evict_move_kernel<8>, grid, block, s, a);
-  if (chunks == 16) return launch_struct(evict_move_kernel<16>, grid, block, s, a);
-  return launch_struct(evict_move_kernel<32>, grid, block, s, a);
+  a.parts = 2;
+  if (chunks == 8) return launch_evict_d<8>(a, layers, batch, s);
+  if (chunks == 16) return launch_evict_d<16>(a, layers, batch, s);
+  return launch_evict_d<32>(a, layers, batch, s);
 }
 
 }  // namespace skv

@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kGammaThreads) void norm_gamma_kernel(NormArgs a) {
 }
 
 // Waves that fill the chip (256 CUs of four SIMDs, some waves each).
-constexpr int kFull = 4096;
+constexpr int kFull = 8192;
 
 // A wave's step: about four rows a lane group, so that the angles are worked out
 // for several rows, but only while the steps fill the chip; with few of them the

@@ -184,8 +184,8 @@ def test_valid_calls_reach_the_device():
 def test_sizes():
     size = skv.speechkv_norm_rope_bwd_workspace_bytes
     for B, S, Hq, Hkv in ((1, 1, 1, 0), (1, 1, 0, 3), (2, 3, 4, 2), (8, 1596, 16, 8), (65535, 200, 64, 8), (1, 2 ** 24 - 1, 1, 1)):
-        for D in (64, 128):  # two sums a block at least, about a thousand blocks at most
-            assert D * 4 <= size(B, S, Hq, Hkv, D) <= 1026 * D * 4
+        for D in (64, 128):  # a sum a block, one block at least and about two thousand at most
+            assert D * 4 <= size(B, S, Hq, Hkv, D) <= 2050 * D * 4
     for bad in ((0, 3, 4, 2, 64), (2, 0, 4, 2, 64), (2, 3, 0, 0, 64), (2, 3, -1, 2, 64), (2, 3, 4, 2, 32),
                 (65535, 1 << 20, 4, 2, 64)):
         assert size(*bad) == 0
