@@ -190,36 +190,57 @@ __device__ __forceinline__ int seen_of(const WeightArgs& a, const Unit& u, int n
   return i < a.num_rows ? min(max(n, 0), u.len) : 0;
 }
 
-// Adds the weights that 16 rows x give the keys k (16 a tile, from key kb on): sum
-// element 4 t + e is of key 16 t + 4 quarter + e, over this lane's rows.
-template <typename T, int D, int kTiles>
+// What a lane needs of its row of a tile: the pieces, the lse, the entries it sees.
+template <typename T, int D>
+struct Row {
+  u32x4_t x[Rows16<T, D>::kPieces];
+  float l;  // in powers of 2
+  int seen;
+  __device__ __forceinline__ void set(float lse, int n) {
+    l = lse * 1.4426950408889634f;
+    seen = l == neg_inf() ? 0 : n;  // (a row that saw nothing)
+  }
+};
+
+// Adds the weights that the rows of n tiles give the keys k (16 a tile, from key kb
+// on): sum element 4 t + e is of key 16 t + 4 quarter + e, over this lane's rows.
+template <typename T, int D, int kTiles, int n>
 __device__ __forceinline__ void add_rows(const WeightArgs& a, const u32x4_t (&k)[kTiles][Rows16<T, D>::kPieces],
-                                         const u32x4_t (&x)[Rows16<T, D>::kPieces], float lse, int seen, int kb,
-                                         int quarter, float (&sum)[4 * kTiles]) {
-  const float l = lse * 1.4426950408889634f;
-  if (l == neg_inf()) seen = 0;  // (a row that saw nothing)
-  f32x4_t st[kTiles];
+                                         const Row<T, D> (&y)[n], int kb, int quarter, float (&sum)[4 * kTiles]) {
+  f32x4_t st[n][kTiles];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) st[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  // (the tiles' sums in turn: a product waits for the one before it of its sum)
+  for (int m = 0; m < n; ++m)
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) st[m][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // (the sums in turn: a product waits for the one before it of its sum)
 #pragma unroll
   for (int p = 0; p < Rows16<T, D>::kPieces; ++p)
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) st[t] = product<T>(k[t][p], x[p], st[t]);
-  if (!__builtin_amdgcn_ballot_w64(seen < kb + 16 * kTiles)) {  // every row sees all keys
+    for (int m = 0; m < n; ++m)
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+      for (int t = 0; t < kTiles; ++t) st[m][t] = product<T>(k[t][p], y[m].x[p], st[m][t]);
+  int least = y[0].seen;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[4 * t + e] += fast_exp2(__builtin_fmaf(st[t][e], a.scale_log2, -l));
+  for (int m = 1; m < n; ++m) least = min(least, y[m].seen);
+  if (!__builtin_amdgcn_ballot_w64(least < kb + 16 * kTiles)) {  // every row sees all keys
+#pragma unroll
+    for (int m = 0; m < n; ++m)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[4 * t + e] += fast_exp2(__builtin_fmaf(st[m][t][e], a.scale_log2, -y[m].l));
   } else {
-    const int most = seen - kb - 4 * quarter;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int m = 0; m < n; ++m) {
+      const int most = y[m].seen - kb - 4 * quarter;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float w = fast_exp2(__builtin_fmaf(st[t][e], a.scale_log2, -l));
-        sum[4 * t + e] += 16 * t + e < most ? w : 0.f;
-      }
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w = fast_exp2(__builtin_fmaf(st[m][t][e], a.scale_log2, -y[m].l));
+          sum[4 * t + e] += 16 * t + e < most ? w : 0.f;
+        }
+    }
   }
 }
 
@@ -295,9 +316,10 @@ __global__ __launch_bounds__(kThreads, 2) void weights_few_kernel(WeightArgs a) 
 #pragma unroll
     for (int rt = 0; rt < kWeightFew; ++rt)
       if (rt < a.row_tiles) {
-        u32x4_t x[L::kPieces];
-        L::read(x, sq + rt * L::kTileBytes, col, quarter);
-        add_rows<T, D, kTiles>(a, k, x, l[rt], seen[rt], kb, quarter, sum);
+        Row<T, D> y[1];
+        L::read(y[0].x, sq + rt * L::kTileBytes, col, quarter);
+        y[0].set(l[rt], seen[rt]);
+        add_rows<T, D, kTiles>(a, k, y, kb, quarter, sum);
       }
     const float total = transposed_sum(sum, lane);
     const int at = key_of<kTiles>(col, quarter);
@@ -317,6 +339,7 @@ __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a
   typedef Rows16<T, D> L;
   constexpr int kKeys = weight_keys(L::kBytes), kTiles = kKeys / 16;
   constexpr int kAhead = L::kBytes > 256 ? 2 : 4;  // row tiles of a wave on their way
+  constexpr int kOnce = kAhead / 2;                // row tiles added at once
   constexpr int kN = L::kTileLoads + 1;            // direct loads of a row tile
   __shared__ __attribute__((aligned(1024))) unsigned char s_row[kManyWaves][kAhead][L::kTileBytes];
   __shared__ int s_info[kManyWaves][kAhead][64];  // lanes 0 .. 31: the rows' lse, 32 .. 63: what they see
@@ -426,15 +449,19 @@ __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a
     for (int j = 0; j < kAhead; ++j) request(tile[j] = next(), j);
     for (int at = 0; at < count; at += kAhead) {
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        wait_vm<(kAhead - 1) * kN>();
-        u32x4_t x[L::kPieces];
-        L::read(x, s_rows + j * L::kTileBytes, col, quarter);
-        const float l = __int_as_float(s_info[wave][j][col]);
-        const int seen = seen_of(a, u, s_info[wave][j][32 + col], tile[j] * queries + in);
+      for (int j = 0; j < kAhead; j += kOnce) {
+        wait_vm<(kAhead - kOnce) * kN>();
+        Row<T, D> y[kOnce];
+#pragma unroll
+        for (int m = 0; m < kOnce; ++m) {
+          L::read(y[m].x, s_rows + (j + m) * L::kTileBytes, col, quarter);
+          const int n = seen_of(a, u, s_info[wave][j + m][32 + col], tile[j + m] * queries + in);
+          y[m].set(__int_as_float(s_info[wave][j + m][col]), at + j + m < count ? n : 0);
+        }
         wait_lds();
-        request(tile[j] = next(), j);  // (always: what waits for the others counts on it)
-        if (at + j < count) add_rows<T, D, kTiles>(a, k, x, l, seen, kb, quarter, sum);
+#pragma unroll
+        for (int m = 0; m < kOnce; ++m) request(tile[j + m] = next(), j + m);  // (always: what waits counts on it)
+        if (at + j < count) add_rows<T, D, kTiles>(a, k, y, kb, quarter, sum);
       }
     }
     wait_vm<0>();
