@@ -29,7 +29,9 @@
  * instead of the one-run spans: speechkv_pool_kv_segments,
  * speechkv_prefill_attn_segments and their backward
  * speechkv_prefill_attn_bwd_segments and speechkv_pool_kv_bwd_segments.
- * Steps of several new tokens over the cache are in speechkv_draft.h.
+ * Steps of several new tokens over the cache are in speechkv_draft.h, norms of
+ * queries and keys with the rotation in speechkv_norm.h, attention over shared
+ * recordings, entry weights and eviction in speechkv_shared.h.
  *
  * Conventions shared by every call
  * --------------------------------

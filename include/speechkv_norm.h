@@ -51,8 +51,8 @@ typedef struct speechkv_heads {
 } speechkv_heads;
 
 /*
- * The norm of a call.  gamma_q, gamma_k: device fp32 [head_dim], or NULL: 1.
- * eps: finite, at least 2^-126.
+ * The norm of a call.  gamma_q, gamma_k: device fp32 [head_dim], 16-byte
+ * aligned, or NULL: 1.  eps: finite, at least 2^-126.
  */
 typedef struct speechkv_head_norm {
   const float* gamma_q;

@@ -86,6 +86,12 @@ bool shared_sizes_bad(int32_t batch, int32_t num_groups, int32_t max_group, int3
          max_group > batch || max_prefix_len < 0 || max_cache_len < 0 || num_splits < 0 || num_splits > kMaxSplits;
 }
 
+// Bytes of [batch][heads][n] values of 4 bytes, or -1 when they do not fit 2^62.
+int64_t rows_bytes(int32_t batch, int32_t heads, int32_t n) {
+  const __int128 bytes = (__int128)batch * heads * n * 4;
+  return bytes < ((__int128)1 << 62) ? (int64_t)bytes : -1;
+}
+
 int64_t capacity_of(const speechkv_paged_kv* c) { return (int64_t)c->max_pages_per_seq * c->page_size; }
 
 KeySource source_of(const speechkv_paged_kv* c, const int32_t* len, int32_t max_len) {
@@ -217,7 +223,8 @@ int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_ro
   a.cache = source_of(cache, cache_len, max_cache_len);
   plan_weights(a, n.dim * n.esz);
   if (((__int128)batch * heads + 7) * a.key_blocks > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
-  const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4, sums = lens * heads * capacity;
+  const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4, sums = rows_bytes(batch, heads, capacity);
+  if (sums < 0) return SPEECHKV_ERR_INVALID_ARG;
   const Region rd[] = {{vq.p, vq.bytes}, {lse, lse_bytes}, {visible, lens * num_rows}, {cache_len, lens},
                        {cache->block_table, table_bytes(cache, batch)}, {cache->k_pages, pool},
                        {weights == weights_out ? nullptr : weights, sums}};
@@ -260,8 +267,9 @@ int speechkv_evict(const speechkv_evict_layer* layers, int32_t num_layers, int32
   // every layer's written buffers against every layer's read ones and against the
   // other written ones (layers may share pools, so K pools are checked against V
   // pools only)
-  const int64_t lens = (int64_t)batch * 4, sums = lens * first.num_kv_heads * capacity;
-  const int64_t lists = lens * first.num_kv_heads * max_keep;
+  const int64_t lens = (int64_t)batch * 4, sums = rows_bytes(batch, first.num_kv_heads, capacity);
+  const int64_t lists = rows_bytes(batch, first.num_kv_heads, max_keep);
+  if (sums < 0 || lists < 0) return SPEECHKV_ERR_INVALID_ARG;
   const int n = num_layers;
   auto k_pool = [&](int i) { return Region{layers[i].cache.k_pages, page_pool_bytes(&layers[i].cache)}; };
   auto v_pool = [&](int i) { return Region{layers[i].cache.v_pages, page_pool_bytes(&layers[i].cache)}; };

@@ -1132,6 +1132,8 @@ def visible_slots(segs, w: int, layer: int, l0: int, mask_mode: int = MASK_WINDO
     segs is [[(text_len, speech_len), ...] per sequence] ([P | T | N] is [(P, T),
     (N, 0)]); returns int32 [B, longest], 0 behind a sequence's last row."""
     w = w if layer >= l0 else 1
+    if w < 1 or mask_mode not in (MASK_WINDOW_END, MASK_WINDOW_START):
+        raise ValueError("a window of at least one frame, and one of the two mask modes")
     rows = []
     for seq in segs:
         seen, slots = [], 0

@@ -144,7 +144,11 @@ def weights(c=None, **kw):
     (dict(q=heads(8, data=at(8) + 8)), E_ARG), (dict(c=cache(head_dim=32)), E_UNS),
     (dict(c=cache(page_size=256, max_pages_per_seq=8388607), max_len=2 ** 31 - 8191, capacity=2 ** 31 - 1), E_UNS),
     (dict(c=cache(page_size=256, max_pages_per_seq=8388607, num_kv_heads=60000), q=heads(8, h=60000), max_len=10 ** 6,
-          capacity=10 ** 6), E_UNS)])
+          capacity=10 ** 6), E_UNS),
+    (dict(c=cache(num_kv_heads=60000, num_pages=1), q=heads(8, h=60000, sb=0, ss=0), batch=65535, rows=1, lb=0, lh=0,
+          capacity=2 ** 31 - 1, max_len=1), E_UNS),  # (blocks before bytes)
+    (dict(c=cache(num_kv_heads=60000, num_pages=1), q=heads(8, h=60000, sb=0, ss=0), batch=65535, rows=1, lb=0, lh=0,
+          capacity=2 ** 31 - 1, max_len=0), E_ARG)])
 def test_weights_rejects(kw, code):
     assert weights(**kw) == code
 
@@ -183,7 +187,9 @@ def evict(layers=None, **kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(keep=None), E_ARG), (dict(keep=at(8) + 2), E_ARG), (dict(batch=0), E_ARG), (dict(batch=65536), E_ARG),
     (dict(max_keep=0), E_ARG), (dict(capacity=0), E_ARG), (dict(first=-1), E_ARG), (dict(recent=-1), E_ARG),
-    (dict(count=0), E_ARG), (dict(count=257), E_ARG), (dict(count=-1), E_ARG)])
+    (dict(count=0), E_ARG), (dict(count=257), E_ARG), (dict(count=-1), E_ARG),
+    (dict(layers=[layer(num_kv_heads=60000)], batch=65535, capacity=2 ** 31 - 1), E_ARG),   # rows past 2^62 bytes
+    (dict(layers=[layer(num_kv_heads=60000)], batch=65535, max_keep=2 ** 31 - 1), E_ARG)])
 def test_evict_rejects(kw, code):
     assert evict(**kw) == code
     assert lib.speechkv_evict(None, 1, 1, at(8), 1, 1, 0, 0, None) == E_ARG
