@@ -15,12 +15,11 @@ using namespace skv;
 constexpr int32_t kMaxLen = INT32_MAX - 8191;
 constexpr int32_t kMaxSplits = 1024;
 
-int row_tiles_of(int64_t rows, int groups) { return (int)((rows + 32 * groups - 1) / (32 * groups)); }
+int row_tiles_of(int64_t rows) { return (int)((rows + kSharedRows - 1) / kSharedRows); }
 
-// How speechkv_shared_attn cuts a call: row groups of a prefix block (1, 2 or 4, of
-// 32 rows each), splits of a prefix and of the own entries.
+// How speechkv_shared_attn cuts a call: splits of a prefix and of the own entries.
 struct SharedPlan {
-  int groups, splits, own_splits;
+  int splits, own_splits;
 };
 
 int64_t tiles_of(int max_len) { return ((int64_t)max_len + kSharedKeys - 1) / kSharedKeys; }
@@ -34,48 +33,44 @@ size_t shared_bytes(int32_t batch, int32_t q_heads, int32_t head_dim, const Shar
 // The estimate is fitted to a sweep on MI355X over 20 shapes of 1 to 64 sequences
 // in 1 to 20 groups, 1 to 8 KV heads of 1 to 8 query heads, prefixes of 126 to 7532
 // and own caches of 10 to 5000 entries, both element types and head sizes; its
-// choice takes 1.3% longer than the best of the candidates on average, 11% at most.
+// choice takes 1.8% longer than the best of the candidates on average, 9% at most.
 // In us:
-//  - a block takes 2, a step of a block's waves over a 128-wide bf16 tile 1.23, 1.11
-//    or 0.88 with 1, 2 or 4 row groups, one of a wave with own entries 1.27; 64-wide
-//    heads take 0.62 of it, fp32 5.1 and 2.5 times; what runs at once is two blocks a
-//    CU (four with 64-wide bf16 heads, one with 128-wide fp32);
-//  - a key is read at 6.5 TB/s, and again by every further row tile at 0.65 of the
-//    cost;
-//  - each partial row is written and read at 3.3 TB/s.
+//  - a block takes 0.3, a step of its four waves over a 128-wide bf16 tile each 1.21,
+//    one of a wave with own entries 1.37; 64-wide heads take 0.58 of it, fp32 5.1 and
+//    2.3 times; what runs at once is two blocks a CU (four with 64-wide bf16 heads, one
+//    with 128-wide fp32), and a full chip takes 1.5 times as long as its blocks alone;
+//  - keys are read at 6.5 TB/s, once;
+//  - each partial row is written and read at 2.3 TB/s.
 SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_heads, int head_dim, int dtype,
                        int max_prefix, int max_len, int splits) {
   const bool f32 = dtype == SPEECHKV_DTYPE_F32, wide = head_dim == 128;
   // members of a group: between the average and the bound
   const double members = 0.5 * (max_group + std::min<double>(max_group, (double)batch / groups));
-  const double units = (double)groups * kv_heads, own_units = (double)batch * kv_heads, row_bytes = head_dim * (f32 ? 4.0 : 2.0);
+  const double units = (double)groups * kv_heads, own_units = (double)batch * kv_heads;
+  const double row_tiles = std::ceil(members * group / kSharedRows), row_bytes = head_dim * (f32 ? 4.0 : 2.0);
   const int64_t tiles = std::max<int64_t>(1, tiles_of(max_prefix)), own = std::max<int64_t>(1, tiles_of(max_len));
   const double slots = 256.0 * (f32 && wide ? 1 : !f32 && !wide ? 4 : 2);
-  const double size = f32 ? (wide ? 5.07 : 2.45) : wide ? 1.0 : 0.62;
+  const double size = f32 ? (wide ? 5.08 : 2.29) : wide ? 1.0 : 0.58;
+  const double read_us = (units * max_prefix + own_units * max_len) * 2 * row_bytes / 6.5e6;
   static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-  SharedPlan best = {1, splits ? splits : 1, 1};
+  SharedPlan best = {splits ? splits : 1, 1};
   double best_us = 1e300;
-  for (int g = 1; g <= 4 && (g == 1 || max_group * (double)group > 16 * g); g *= 2) {
-    const double step_us = (g == 1 ? 1.23 : g == 2 ? 1.11 : 0.88) * size;
-    const double row_tiles = std::ceil(members * group / (32.0 * g));
-    for (int count : counts) {
-      const int s = splits ? splits : count;
-      if (!splits && s > tiles) break;
-      const double block_us = 1.98 + step_us * (double)(((tiles + s - 1) / s * g + 3) / 4);
-      for (int o : counts) {
-        if (o > own || o > 32) break;
-        const double own_us = 1.98 + 1.27 * size * (double)((own + o - 1) / o);
-        const double all_us = 1.12 * (units * row_tiles * s * block_us + std::ceil(own_units * o / 4) * own_us) / slots;
-        const double read_us = (units * max_prefix * (1 + 0.65 * (row_tiles - 1)) + own_units * max_len) * 2 * row_bytes / 6.5e6;
-        const double us = std::max({block_us, own_us, all_us, 1.98 + read_us}) + 0.2 * all_us +
-                          own_units * group * (s + o) * head_dim * 8 / 3.27e6;
-        if (us < best_us) {
-          best_us = us;
-          best = {g, s, o};
-        }
+  for (int count : counts) {
+    const int s = splits ? splits : count;
+    if (!splits && s > tiles) break;
+    const double block_us = 0.31 + 1.21 * size * (double)(((tiles + s - 1) / s + 3) / 4);
+    for (int o : counts) {
+      if (o > own || o > 32) break;
+      const double own_us = 0.31 + 1.37 * size * (double)((own + o - 1) / o);
+      const double all_us = 1.5 * (units * row_tiles * s * block_us + std::ceil(own_units * o / 4) * own_us) / slots;
+      const double us = std::max({block_us, own_us, all_us, 0.31 + read_us}) +
+                        own_units * group * (s + o) * head_dim * 8 / 2.34e6;
+      if (us < best_us) {
+        best_us = us;
+        best = {s, o};
       }
-      if (splits) break;
     }
+    if (splits) break;
   }
   return best;
 }
@@ -155,8 +150,9 @@ int speechkv_shared_attn(const void* q, int32_t batch, int32_t num_q_heads, cons
                                       max_cache_len, num_splits);
   const size_t need = shared_bytes(batch, num_q_heads, D, plan);
   if (!workspace || workspace_bytes < need || !aligned16(workspace)) return SPEECHKV_ERR_WORKSPACE;
-  const int row_tiles = row_tiles_of((int64_t)max_group * group, plan.groups);
-  const __int128 blocks = (__int128)num_groups * heads * plan.splits * row_tiles + (__int128)batch * heads * plan.own_splits;
+  const int row_tiles = row_tiles_of((int64_t)max_group * group);
+  const __int128 blocks = ((__int128)num_groups * heads * plan.splits + 7) * row_tiles +
+                          (__int128)batch * heads * plan.own_splits;
   const int64_t merged = (int64_t)batch * num_q_heads / (256 / (D / 4)) + 1;
   if (blocks > kMaxBlocks || merged > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
   const int64_t qo = (int64_t)batch * num_q_heads * D * elt_size(cache->dtype), lens = (int64_t)batch * 4;
@@ -178,7 +174,6 @@ int speechkv_shared_attn(const void* q, int32_t batch, int32_t num_q_heads, cons
   a.num_q_heads = num_q_heads;
   a.group_shift = log2_exact(group);
   a.scale_log2 = scale * 1.4426950408889634f;
-  a.row_groups = plan.groups;
   a.row_tiles = row_tiles;
   a.prefix_splits = plan.splits;
   a.own_splits = plan.own_splits;

@@ -23,11 +23,11 @@ struct SharedArgs {
   int batch, groups, max_group;
   int num_q_heads, group_shift;  // log2 of the query heads per KV head
   float scale_log2;              // scale * log2(e)
-  int row_groups;                // of a prefix block: 1, 2 or 4 (of 32 rows each)
   int row_tiles;                 // prefix blocks that share a (group, KV head)'s rows
   int prefix_splits, own_splits;
   int prefix_tiles, own_tiles;   // key tiles of a split, from the host's bounds
-  int prefix_blocks;             // (set by the launcher, as the divisors)
+  int prefix_units;              // (group, KV head)s times splits (set by the launcher,
+  int prefix_blocks;             // as their blocks and the divisors)
   FastDivide by_row_tiles, by_prefix_splits, by_own_splits, by_heads;
   void* out;
   float* lse;    // may be null
@@ -87,6 +87,7 @@ static_assert(sizeof(EvictArgs) <= 4096, "kernel arguments");
 hipError_t launch_shared(const SharedArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_shared_merge(const SharedArgs& a, int dtype, int head_dim, hipStream_t s);
 constexpr int kSharedKeys = 32;  // keys of a tile
+constexpr int kSharedRows = 32;  // rows of a prefix block
 hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, int dtype, int head_dim, int layers, int batch, hipStream_t s);
 

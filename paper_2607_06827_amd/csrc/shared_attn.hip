@@ -5,18 +5,21 @@
 // G query heads of its group, are one matrix and the prefix is read once for all
 // of them; what they have of their own is read once each, with G rows.  Both are
 // partial results of the same softmax: blocks of one launch compute them (prefix
-// blocks: a group, KV head, range of its keys and up to 128 rows; the waves of own
+// blocks: a group, KV head, range of its keys and 32 rows; the waves of own
 // blocks: a sequence, KV head and range of its keys each), and a second launch merges a row's
 // partials by log-sum-exp, in a fixed order.
 //
-// A block of four waves takes 32, 64 or 128 rows (kGroups = 1, 2 or 4 row groups of
-// 32, a wave each) and a range of keys in tiles of 32; with fewer than four row
-// groups the waves split the tiles between them.  A wave holds its query rows in
-// registers and per tile computes S^T = K Q^T and O^T += V^T P^T on the 32x32
+// A block of four waves takes 32 rows and a range of keys in tiles of 32, which the
+// waves deal out (of its own entries a wave has a whole range); each holds the query
+// rows in registers and per tile computes S^T = K Q^T and O^T += V^T P^T on the 32x32
 // matrix products (tile_attn.hpp) with the online softmax between them.  Tiles go
-// from the paged cache straight into LDS.  With one row group every wave streams its
-// own tiles with no barrier; with more the waves of a stream load a tile together,
-// one tile ahead, one barrier a tile.
+// from the paged cache straight into LDS, into a K and a V buffer of the wave's own,
+// the next K requested as soon as S^T is there, the next V as soon as O^T is: no
+// barrier.  More than 32 rows are more blocks that read the same keys, side by side
+// on one XCD and out of its L2 (on different XCDs HBM gives the keys to each: 64
+// questions about 7532 entries 24 us, 21 so).  Blocks of 64 or 128 rows, whose waves
+// share a tile and a barrier, are slower (23 and 25 us), also with four tiles on their
+// way, and so are blocks of eight waves.
 //
 // Every row of a block sees the same keys, so keys that are not there (past the
 // last, or without a page) are masked for all: their logits become -inf and their
@@ -34,8 +37,8 @@ namespace {
 constexpr int kWaves = 4;
 static_assert(kSharedKeys == kKeys, "the tile that the host cuts splits by");
 
-// What a block attends: rows (from `first` on, `rows` of them, of which it has
-// 32 kGroups from `row0` on) and keys.
+// What a block, or a wave, attends: rows (`rows` of them, of which it has 32 from
+// `row0` on) and keys.
 struct Job {
   const KeySource* src;
   int entry;           // row of the block table
@@ -47,19 +50,17 @@ struct Job {
   int part;            // which partial result it is
 };
 
-// kOnce: no other block reads its keys.  kAlone: every wave has a job of its own,
-// of at most 32 rows (kGroups = 1), and meets no barrier.
-template <typename T, int D, int kGroups, bool kOnce, bool kAlone>
+// kOnce: no other block reads its keys.  kAlone: every wave has a job of its own and
+// meets no barrier.
+template <typename T, int D, bool kOnce, bool kAlone>
 __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsigned char* s_tile, float (*s_m)[32],
                                        float (*s_l)[32]) {
   typedef Tile<T, D> L;
-  static_assert(!kAlone || kGroups == 1, "a wave's rows");
-  constexpr int kStreams = kAlone ? 1 : kWaves / kGroups;
-  constexpr int kShare = kKeys / kGroups, kRuns = kShare / 8;  // rows, runs of 8 rows that a wave loads
-  constexpr int kLoadsPerWave = L::kLoads / kGroups, kVm = 2 * kLoadsPerWave;
-  static_assert(L::kLoads % kGroups == 0 && kVm < 63, "vector-memory counter");
+  constexpr int kStreams = kAlone ? 1 : kWaves;  // waves that the tiles are dealt to
+  constexpr int kRuns = kKeys / 8;               // runs of 8 rows of a tile
+  static_assert(L::kLoads < 63, "vector-memory counter");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rg = wave % kGroups, stream = kAlone ? 0 : wave / kGroups;
+  const int stream = kAlone ? 0 : wave;
   const int col = lane & 31, hg = lane >> 5;
   const int parts = a.prefix_splits + a.own_splits, gshift = a.group_shift, gmask = (1 << gshift) - 1;
   const KeySource& src = *job.src;
@@ -71,7 +72,8 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
   };
   const int t_end = min(job.tile1, (job.keys + kKeys - 1) / kKeys), last = job.keys - 1;
   if (job.tile0 >= t_end) {  // nothing here: the merge passes over it
-    for (int r = job.row0 + (kAlone ? lane : tid); r < min(job.rows, job.row0 + 32 * kGroups); r += kWaves * 64) {
+    const int r = job.row0 + (kAlone ? lane : tid);
+    if (r < min(job.rows, job.row0 + 32)) {
       const int64_t at = out_row(r) * parts + job.part;
       a.ws_ml[2 * at] = neg_inf();
       a.ws_ml[2 * at + 1] = 0.f;
@@ -79,7 +81,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
     return;
   }
 
-  const int r = job.row0 + rg * 32 + col;  // this lane's row
+  const int r = job.row0 + col;  // this lane's row
   u32x4_t q[L::kFrags];
   {
     const char* row = static_cast<const char*>(a.q) + out_row(min(r, job.rows - 1)) * L::kRowBytes + 16 * hg;
@@ -146,7 +148,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
     Entries x;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) {
-      const int from = lane0 + rg * kRuns + i;
+      const int from = lane0 + i;
       x.at[i] = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(run_hi, from) << 32 |
                 (uint32_t)__builtin_amdgcn_readlane(run_lo, from);
     }
@@ -154,28 +156,28 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
     x.present = ((ok * 0x00204081u) & 0x01010101u) * 0xffu;  // each bit to a byte
     return x;
   };
-  const uint32_t lane_k = lrow * L::kRowBytes + ((lpos ^ L::k(lrow) ^ L::k(rg * kShare)) << 4);
+  const uint32_t lane_k = lrow * L::kRowBytes + ((lpos ^ L::k(lrow)) << 4);
   const uint32_t lane_v = lrow * L::kRowBytes + ((lpos ^ L::v(lrow)) << 4);
-  // This wave's share of tile t into LDS at dst (K or V).  In the last tile, rows
+  // Tile t into LDS at dst (K or V).  In the last tile, rows
   // past the last key read that key's row.
   auto load = [&](int t, const Entries& x, uint32_t dst, bool is_v) __attribute__((always_inline)) {
     auto move = [&](uint64_t at, uint32_t off, int in) __attribute__((always_inline)) {
       if (is_v) at += v_minus_k;
-      const uint32_t to = __builtin_amdgcn_readfirstlane(dst + (rg * kShare + in) * L::kRowBytes);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(dst + in * L::kRowBytes);
       if constexpr (kOnce) lds_dma16_nt((const void*)at, off, to);
       else lds_dma16((const void*)at, off, to);
     };
     if (t * kKeys + kKeys <= job.keys) {
 #pragma unroll
-      for (int i = 0; i < kLoadsPerWave; ++i) {
+      for (int i = 0; i < L::kLoads; ++i) {
         const int in = i * L::kRowsPerLoad;  // (a constant)
         const uint32_t swz = (is_v ? L::v(in) : L::k(in)) << 4;
         move(x.at[in / 8], ((is_v ? lane_v : lane_k) ^ swz) + (in & 7) * L::kRowBytes, in);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kLoadsPerWave; ++i) {
-        const int in = i * L::kRowsPerLoad, row = rg * kShare + in + lrow;
+      for (int i = 0; i < L::kLoads; ++i) {
+        const int in = i * L::kRowsPerLoad, row = in + lrow;
         const int swz = is_v ? L::v(row) : L::k(row);
         const int to = t * kKeys + (row | 7) > last ? min((in & 7) + lrow, last & 7) : (in & 7) + lrow;
         move(x.at[in / 8], to * L::kRowBytes + ((lpos ^ swz) << 4), in);
@@ -233,8 +235,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
     l_run += sum;
   };
   // Values of keys that are not there become 0 in LDS: 0 times what lies there may
-  // be NaN.  (Waves that share a tile all write the same zeros, each before its
-  // own reads.)
+  // be NaN.
   auto clear_missing = [&](uint32_t sv, uint32_t bits) __attribute__((always_inline)) {
     typedef __attribute__((address_space(3))) u32x4_t* lds_ptr;
 #pragma nounroll
@@ -243,71 +244,40 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
     wait_lds();
   };
 
-  if constexpr (kGroups == 1) {
-    const uint32_t sk = lds0 + wave * 2 * L::kBytes, sv = sk + L::kBytes;
-    if (t_first < t_end) {
-      int t = t_first, step = 0;
-      Entries x = entries(0);
-      load(t, x, sk, false);
+  const uint32_t sk = lds0 + wave * 2 * L::kBytes, sv = sk + L::kBytes;
+  if (t_first < t_end) {
+    int t = t_first, step = 0;
+    Entries x = entries(0);
+    load(t, x, sk, false);
+    load(t, x, sv, true);
+    wait_vm<L::kLoads>();
+    while (true) {
+      const bool more = t + kStreams < t_end;
+      const uint32_t bits = bits_of(t, x.present);
+      const f32x16_t st = scores<T, D>(sk, q, lane);
+      wait_lds();
+      ++step;
+      if (more) {
+        x = entries(step);
+        load(t + kStreams, x, sk, false);
+      }
+      float p[16];
+      softmax(st, bits, p);
+      if (more) wait_vm<L::kLoads>();
+      else wait_vm<0>();
+      if (bits != ~0u) clear_missing(sv, bits);
+      add_values<T, D>(sv, p, o, lane);
+      if (!more) break;
+      wait_lds();
+      t += kStreams;
       load(t, x, sv, true);
-      wait_vm<kVm / 2>();
-      while (true) {
-        const bool more = t + kStreams < t_end;
-        const uint32_t bits = bits_of(t, x.present);
-        const f32x16_t st = scores<T, D>(sk, q, lane);
-        wait_lds();
-        ++step;
-        if (more) {
-          x = entries(step);
-          load(t + kStreams, x, sk, false);
-        }
-        float p[16];
-        softmax(st, bits, p);
-        if (more) wait_vm<kVm / 2>();
-        else wait_vm<0>();
-        if (bits != ~0u) clear_missing(sv, bits);
-        add_values<T, D>(sv, p, o, lane);
-        if (!more) break;
-        wait_lds();
-        t += kStreams;
-        load(t, x, sv, true);
-        wait_vm<kVm / 2>();
-      }
-    }
-  } else {
-    const uint32_t base = lds0 + stream * 4 * L::kBytes;
-    const int steps = (t_end - job.tile0 + kStreams - 1) / kStreams;
-    Entries x;
-    x.present = 0;
-    auto request = [&](int step) __attribute__((always_inline)) {
-      const int t = t_first + step * kStreams;
-      if (t >= t_end) return;
-      const uint32_t dst = base + (uint32_t)(step & 1) * 2 * L::kBytes;
-      x = entries(step);
-      load(t, x, dst, false);
-      load(t, x, dst + L::kBytes, true);
-    };
-    request(0);
-    for (int step = 0; step < steps; ++step) {
-      bare_barrier<0>();  // this step's tile has landed in every wave's part
-      const int t = t_first + step * kStreams;
-      const uint32_t present = x.present;
-      request(step + 1);
-      if (t < t_end) {
-        const uint32_t sk = base + (uint32_t)(step & 1) * 2 * L::kBytes, sv = sk + L::kBytes;
-        const uint32_t bits = bits_of(t, present);
-        const f32x16_t st = scores<T, D>(sk, q, lane);
-        float p[16];
-        softmax(st, bits, p);
-        if (bits != ~0u) clear_missing(sv, bits);
-        add_values<T, D>(sv, p, o, lane);
-      }
+      wait_vm<L::kLoads>();
     }
   }
   if constexpr (!kAlone) __syncthreads();  // every wave is done with the tiles, and no load is in flight
 
   const float l_tot = partner_sum(l_run);
-  if constexpr (kStreams == 1) {
+  if constexpr (kAlone) {
     if (r >= job.rows) return;
     const int64_t at = out_row(r) * parts + job.part;
 #pragma unroll
@@ -321,7 +291,7 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
       a.ws_ml[2 * at + 1] = l_tot;
     }
   } else {
-    // the streams' rows through LDS: wave w's 32 x D sums at s_o + 32 w D, 16-byte
+    // the waves' rows through LDS: wave w's 32 x D sums at s_o + 32 w D, 16-byte
     // chunks swizzled by the row
     float* const s_o = reinterpret_cast<float*>(s_tile);
     constexpr int kO = D / 4;  // chunks of an output row
@@ -336,21 +306,20 @@ __device__ __forceinline__ void attend(const SharedArgs& a, const Job& job, unsi
         *reinterpret_cast<f32x4_t*>(s_o + (wave * 32 + col) * D + (((8 * db + 2 * ig + hg) ^ (col & (kO - 1))) << 2)) =
             f32x4_t{o[db][4 * ig], o[db][4 * ig + 1], o[db][4 * ig + 2], o[db][4 * ig + 3]};
     __syncthreads();
-    for (int it = tid; it < 32 * kGroups * kO; it += kWaves * 64) {
-      const int row = it / kO, ch = it % kO, rr = row & 31, rw = row >> 5;
+    for (int it = tid; it < 32 * kO; it += kWaves * 64) {
+      const int row = it / kO, ch = it % kO;
       if (job.row0 + row >= job.rows) continue;
       float M = neg_inf();
 #pragma unroll
-      for (int s = 0; s < kStreams; ++s) M = fmaxf(M, s_m[s * kGroups + rw][rr]);
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row]);
       f32x4_t num = {0.f, 0.f, 0.f, 0.f};
       float den = 0.f;
 #pragma unroll
-      for (int s = 0; s < kStreams; ++s) {
-        const int w = s * kGroups + rw;
-        const float ms = s_m[w][rr];
+      for (int w = 0; w < kWaves; ++w) {
+        const float ms = s_m[w][row];
         const float f = ms == neg_inf() ? 0.f : fast_exp2(ms - M);
-        den += f * s_l[w][rr];
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s_o + (w * 32 + rr) * D + ((ch ^ (rr & (kO - 1))) << 2));
+        den += f * s_l[w][row];
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(s_o + (w * 32 + row) * D + ((ch ^ (row & (kO - 1))) << 2));
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] += f * x[e];
       }
@@ -374,17 +343,19 @@ __device__ __forceinline__ int keys_of(const KeySource& src, int entry) {
   return (int)min((int64_t)min(max(src.len[entry], 0), src.max_len), (int64_t)src.pv.max_pages << src.pv.page_shift);
 }
 
-template <typename T, int D, int kGroups, bool kOnce>
+template <typename T, int D, bool kOnce>
 __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 || D == 64 ? 2 : 1)) void shared_kernel(SharedArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char s_tile[kWaves * 2 * Tile<T, D>::kBytes];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
-  static_assert(sizeof(s_tile) >= (kGroups == 1 ? 1 : 2) * (kWaves / kGroups) * 2 * Tile<T, D>::kBytes &&
-                    sizeof(s_tile) >= kWaves * 32 * D * (kGroups == kWaves ? 0 : 4),
-                "two buffers a stream, or one a wave; the streams' sums");
+  static_assert(sizeof(s_tile) >= kWaves * 32 * D * 4, "the waves' sums");
   Job job;
   if ((int)blockIdx.x < a.prefix_blocks) {
     int unit, row_tile, pair, split, j, first, count;
-    a.by_row_tiles.divide(blockIdx.x, unit, row_tile);
+    // the row tiles of a unit read the same keys: they follow each other on one XCD
+    // (block index mod 8) and its L2
+    a.by_row_tiles.divide((int)(blockIdx.x >> 3), unit, row_tile);
+    unit = unit * 8 + (int)(blockIdx.x & 7);
+    if (unit >= a.prefix_units) return;
     a.by_prefix_splits.divide(unit, pair, split);
     a.by_heads.divide(pair, j, job.g);
     members(a, j, first, count);
@@ -392,13 +363,13 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 || D == 64 ? 2 : 1)) v
     job.entry = j;
     job.first_b = first;
     job.rows = count << a.group_shift;
-    job.row0 = row_tile * 32 * kGroups;
+    job.row0 = row_tile * kSharedRows;
     if (job.row0 >= job.rows) return;
     job.keys = keys_of(a.prefix, j);
     job.tile0 = split * a.prefix_tiles;
     job.tile1 = job.tile0 + a.prefix_tiles;
     job.part = split;
-    attend<T, D, kGroups, kOnce, false>(a, job, s_tile, s_m, s_l);
+    attend<T, D, kOnce, false>(a, job, s_tile, s_m, s_l);
   } else {
     // a (sequence, KV head) and split a wave
     int pair, split, b;
@@ -414,7 +385,7 @@ __global__ __launch_bounds__(kWaves * 64, (sizeof(T) == 2 || D == 64 ? 2 : 1)) v
     job.tile0 = split * a.own_tiles;
     job.tile1 = job.tile0 + a.own_tiles;
     job.part = a.prefix_splits + split;
-    attend<T, D, 1, true, true>(a, job, s_tile, s_m, s_l);
+    attend<T, D, true, true>(a, job, s_tile, s_m, s_l);
   }
 }
 
@@ -496,17 +467,12 @@ hipError_t launch_shared_d(const SharedArgs& args, hipStream_t s) {
   a.by_prefix_splits = FastDivide(a.prefix_splits);
   a.by_own_splits = FastDivide(a.own_splits);
   a.by_heads = FastDivide(heads);
-  a.prefix_blocks = a.groups * heads * a.prefix_splits * a.row_tiles;
+  a.prefix_units = a.groups * heads * a.prefix_splits;
+  a.prefix_blocks = (a.prefix_units + 7) / 8 * 8 * a.row_tiles;
   const int64_t own_units = (int64_t)a.batch * heads * a.own_splits;
   const dim3 grid((uint32_t)(a.prefix_blocks + (own_units + kWaves - 1) / kWaves)), block(kWaves * 64);
-  auto launch = [&](auto groups) {
-    constexpr int G = decltype(groups)::value;
-    return a.row_tiles == 1 ? launch_struct(shared_kernel<T, D, G, true>, grid, block, s, a)
-                            : launch_struct(shared_kernel<T, D, G, false>, grid, block, s, a);
-  };
-  if (a.row_groups == 1) return launch(std::integral_constant<int, 1>());
-  if (a.row_groups == 2) return launch(std::integral_constant<int, 2>());
-  return launch(std::integral_constant<int, 4>());
+  return a.row_tiles == 1 ? launch_struct(shared_kernel<T, D, true>, grid, block, s, a)
+                          : launch_struct(shared_kernel<T, D, false>, grid, block, s, a);
 }
 
 hipError_t launch_shared(const SharedArgs& a, int dtype, int head_dim, hipStream_t s) {
