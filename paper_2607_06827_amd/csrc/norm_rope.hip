@@ -15,6 +15,14 @@
 // far positions lose nothing.
 //
 // Sums, norms, the rotation and gradients are fp32; each output is rounded once.
+//
+// Bound by HBM: the prompts of 8 users (12768 tokens of 16 + 8 heads, bf16) take 33 us
+// forward, 157 MB at 4.8 TB/s, and 51.5 backward, 235 MB at 4.6 (a large copy reaches
+// 5.1); the counters give the bytes of the rows, no more.  What small calls wait for is
+// the chain of loads: row counts, rows, and backward the sums' second launch.  With a
+// block of 256 threads a token and two barriers for its angles the backward took 142
+// us; with more tokens a step both take 1 to 3 us longer, and non-temporal stores,
+// unrolled rows or fewer registers change nothing.
 #include <algorithm>
 
 #include "kernels_norm.hpp"

@@ -490,6 +490,55 @@ def test_evict_captured_and_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
+# ------------------------------------------------------------------ far away
+
+def test_offsets_past_32_bits():
+    """Pages and rows that lie more than 2^32 bytes into their tensors give what the
+    same values near the start give."""
+    Hq, Hkv, D, ps, pages = 4, 2, 128, 256, 34000  # 4.5 GB a pool
+    k, v = (torch.empty((pages, Hkv, ps, D), dtype=BF, device=DEV) for _ in range(2))
+    far, near = [pages - 1, 2, pages - 40, pages - 3], [0, 1, 2, 3]
+    nk, nv = (inputs.normal((4, Hkv, ps, D), 30 + i, dtype=BF).to(DEV) for i in range(2))
+    for i, p in enumerate(far):
+        k[p], v[p] = nk[i], nv[i]
+    L = 4 * ps - 9
+    results = []
+    for kk, vv, t in ((k, v, far), (nk, nv, near)):
+        c = skv.PagedKV(kk, vv, i32([t]))
+        mine = skv.PagedKV(kk, vv, i32([t[1:2], t[2:3], t[3:]]))
+        q = inputs.normal((3, Hq, D), 40, dtype=BF).to(DEV)
+        out, lse = torch.empty_like(q), torch.empty(3, Hq, device=DEV)
+        need = skv.speechkv_shared_workspace_bytes(3, 1, 3, Hq, Hkv, D, L, 200)
+        skv.speechkv_shared_attn(q, c, i32([L]), L, i32([0, 3]), 3, mine, i32([200, 3, 77]), 200, out, lse=lse,
+                                 workspace=torch.empty(need, dtype=torch.uint8, device=DEV))
+        gathered = []
+        for rows in (q[:, None], q[:, None].expand(3, 20, Hq, D)):  # few rows, many rows
+            n = rows.shape[1]
+            w = torch.empty(1, Hkv, L, device=DEV)
+            skv.speechkv_attn_weights(rows.reshape(1, 3 * n, Hq, D), lse[:, None].expand(3, n, Hq).reshape(3 * n, Hq).t()[None],
+                                      c, i32([L]), L, w, visible=i32([[L - i for i in range(3 * n)]]))
+            gathered.append(w)
+        kept, n_out = torch.zeros((1, Hkv, 500), dtype=torch.int32, device=DEV), i32([0])
+        skv.speechkv_evict(skv.EvictStack([c], [i32([L])], [n_out], [gathered[1]], [torch.empty_like(w)], [kept]), i32([500]),
+                           4, 8)
+        new = inputs.normal((1, 7, Hq + 2 * Hkv, D), 50, dtype=BF).to(DEV)
+        skv.speechkv_norm_append_kv(None, new[:, :, Hq:Hq + Hkv], new[:, :, Hq + Hkv:], c, n_out)
+        table = c.block_table[0, :2].long()
+        results.append([out, lse, *gathered, kept, kk[table].clone(), vv[table].clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    # rows of a tensor that ends 4.5 GB behind its start, read and written in place
+    flat = k.view(-1)
+    rows = torch.as_strided(flat, (2, 3, 2, D), (flat.numel() - 3 * 2 * D, 2 * D, D, 1))
+    x = inputs.normal((2, 3, 2, D), 60, dtype=BF).to(DEV)
+    rows.copy_(x)
+    want, dx, dwant = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    skv.speechkv_norm_rope(x, None, want, None)
+    skv.speechkv_norm_rope_bwd(x, None, want, None, dwant, None)
+    skv.speechkv_norm_rope_bwd(rows, None, want, None, dx, None)
+    skv.speechkv_norm_rope(rows, None, rows, None)
+    assert torch.equal(rows, want) and torch.equal(dx, dwant)
+
+
 # ------------------------------------------------------------- all together
 
 def test_questions_about_a_recording_within_a_budget():
