@@ -30,6 +30,9 @@ CASES = [
     (BF, 128, 5, 3, 2, 11, 64, False, 2, None, "fused", -70000, False, False),
     (F32, 64, 1, 1, 2, 3, 64, False, 16, None, "dense", 5, False, False),
     (BF, 64, 64, 8, 5, 301, 64, False, 3, [301, 0, 17, 300, 1], "fused", 1000, True, True),
+    # many tokens: two and eight of them a step
+    (F32, 128, 1, 1, 9, 2000, 128, True, 1, None, "fused", 7, True, True),
+    (BF, 64, 2, 1, 33, 4000, 32, False, 2, [4000 - 119 * i for i in range(33)], "dense", 0, True, True),
 ]
 
 

@@ -229,6 +229,9 @@ WEIGHTS = [
     (BF, 64, 64, 8, 128, [500], 17, "last"),
     (F32, 128, 8, 1, 256, [1000, 999], 2, "last"),
     (BF, 128, 2, 1, 16, [7, 3], 300, "last"),  # rows that see nothing
+    (BF, 64, 8, 8, 16, [9000, 4001, 17], 1, "last"),  # several steps of keys a wave
+    (BF, 64, 8, 1, 16, [90], 1100, "any"),  # more row tiles than are looked through at once
+    (F32, 128, 8, 1, 16, [70], 1030, "last"),
 ]
 
 
@@ -351,6 +354,9 @@ EVICT = [
     (BF, 128, 2, 16, [90] * 3, [40, 41, 90], 2, 5, 70),
     (BF, 64, 1, 16, [5000], [2500], 10, 100, 1),
     (BF, 128, 1, 32, [40, 9], [1, 8], 0, 1, 1),
+    # choice and moves in one kernel; weights that stay in registers, and that do not
+    (BF, 64, 8, 16, [2500] + [300 + 7 * i for i in range(15)], [200 + 20 * i for i in range(16)], 4, 16, 5),
+    (F32, 128, 16, 8, [70, 20], [40, 30], 2, 3, 33),
 ]
 
 
