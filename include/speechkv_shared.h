@@ -133,7 +133,7 @@ size_t speechkv_shared_workspace_bytes(int32_t batch, int32_t num_groups, int32_
  * capacity       entries of a row of weights (>= 1).
  * Errors: INVALID_ARG, UNSUPPORTED (also where the launch would need 2^24
  *         blocks or more, or for caches of 2^31 - 8191 entries and more), HIP;
- *         ALIAS when weights_out overlaps anything read but for weights = 
+ *         ALIAS when weights_out overlaps anything read but for weights =
  *         weights_out.
  */
 int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_rows,
@@ -163,7 +163,7 @@ typedef struct speechkv_evict_layer {
 
 /*
  * speechkv_evict - shortens caches to the entries that gathered most weight, in
- * all layers with two launches (per 32 layers).
+ * all layers with one or two launches (per 32 layers).
  *
  * For every layer, sequence b and KV head g, with L = cache_len[b]:
  *   n = min(L, keep_len[b]) entries stay: the first f = min(num_first, n), the

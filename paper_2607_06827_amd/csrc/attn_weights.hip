@@ -23,8 +23,8 @@
 // the first keys, which every row sees, set the time; six waves and two blocks a CU 38.
 #include <algorithm>
 
-#include "attn_mfma.hpp"
 #include "kernels_shared.hpp"
+#include "tile_attn.hpp"
 
 namespace skv {
 
@@ -61,18 +61,6 @@ __device__ __forceinline__ void lds_dma16_from(const void* p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(p), "s"(lds) : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
-}
-
-template <int kVm>
-__device__ __forceinline__ void wait_vm() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt vmcnt(%0)" : : "i"(kVm) : "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-__device__ __forceinline__ void wait_lds() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <typename T>

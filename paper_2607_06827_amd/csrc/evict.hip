@@ -2,7 +2,7 @@
 //
 // Of a (layer, sequence, KV head)'s L entries n stay: the first, the last, and of
 // those between them the m heaviest.  A block finds the m-th largest weight digit
-// by digit (weights as whole numbers in the order of the numbers; four passes of
+// by digit (weights as whole numbers in the order of the numbers; up to four passes of
 // 8 bits over the row, a histogram each), which needs no sort; entries above it
 // stay, and of those equal to it the lowest slots.  A second pass over the row
 // counts who stays before each entry, in order, and writes the kept slots and
@@ -18,7 +18,8 @@
 // non-temporally (140 us without), eight pieces a thread (133 with 16: fewer blocks run
 // at once).  From 512 rows on one kernel chooses and moves (134 us as two launches, as
 // the choice alone, all latency, takes 15); one layer of one sequence has 8 and takes
-// 6.8 and 4.7 us as two, whose moves have four times the blocks.
+// 5.7 and 4.9 us as two, whose moves have four times the blocks (6.8 with all four
+// passes, though fewer settle it).
 #include <algorithm>
 
 #include "kernels_shared.hpp"
@@ -122,7 +123,8 @@ __device__ __forceinline__ void choose(const EvictArgs& a, const EvictLayer& y, 
         for (int k = 3; k >= 0; --k) {
           if (above < left && left <= above + mine[k]) {
             s.digit = 4 * lane + k;
-            s.left = left - above;
+            // (all with this digit stay: none of their lower digits matters)
+            s.left = mine[k] == left - above ? INT32_MAX : left - above;
           }
           above += mine[k];
         }
@@ -130,6 +132,7 @@ __device__ __forceinline__ void choose(const EvictArgs& a, const EvictLayer& y, 
       __syncthreads();
       least |= (uint32_t)s.digit << shift;
       left = s.left;
+      if (left == INT32_MAX) break;
     }
   }
   // `left` of those equal to `least` stay, the lowest slots first
