@@ -194,10 +194,10 @@ typedef struct speechkv_evict_layer {
  * max_keep       entries of a row of kept (>= 1), a bound on keep_len.
  * capacity       entries of a row of weights (>= 1), a bound on cache_len.
  * num_first, num_recent  >= 0.
- * Errors: INVALID_ARG, UNSUPPORTED, HIP; ALIAS when a buffer written (pools,
- *         weights_out, kept, cache_len_out) overlaps one read or another
- *         written, of any layers (but for pools of the same kind, and weights =
- *         weights_out).
+ * Errors: INVALID_ARG, HIP; UNSUPPORTED also for a capacity of 2^31 - 8191 and
+ *         more; ALIAS when a buffer written (pools, weights_out, kept,
+ *         cache_len_out) overlaps one read or another written, of any layers
+ *         (but for pools of the same kind, and weights = weights_out).
  */
 int speechkv_evict(const speechkv_evict_layer* layers, int32_t num_layers, int32_t batch,
                    const int32_t* keep_len, int32_t max_keep, int32_t capacity,

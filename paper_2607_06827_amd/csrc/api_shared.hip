@@ -265,6 +265,7 @@ int speechkv_evict(const speechkv_evict_layer* layers, int32_t num_layers, int32
   const int64_t lens = (int64_t)batch * 4, sums = rows_bytes(batch, first.num_kv_heads, capacity);
   const int64_t lists = rows_bytes(batch, first.num_kv_heads, max_keep);
   if (sums < 0 || lists < 0) return SPEECHKV_ERR_INVALID_ARG;
+  if (capacity > kMaxLen) return SPEECHKV_ERR_UNSUPPORTED;
   const int n = num_layers;
   auto k_pool = [&](int i) { return Region{layers[i].cache.k_pages, page_pool_bytes(&layers[i].cache)}; };
   auto v_pool = [&](int i) { return Region{layers[i].cache.v_pages, page_pool_bytes(&layers[i].cache)}; };

@@ -215,6 +215,11 @@ def test_evict_rejects_layers(layers, code):
     assert evict(layers) == code
 
 
+def test_evict_refuses_lengths_past_31_bits_with_a_stretch():
+    assert evict([layer(num_kv_heads=1)], batch=1, capacity=2 ** 31 - 8191) == E_UNS
+    assert evict([layer(num_kv_heads=1)], batch=1, capacity=2 ** 31 - 1) == E_UNS
+
+
 @NO_GPU
 def test_evict_valid_calls_reach_the_device():
     assert evict() == E_HIP and evict([layer(out=at(23)), layer(1, page_size=64, max_pages_per_seq=3)]) == E_HIP
