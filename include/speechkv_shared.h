@@ -131,8 +131,8 @@ size_t speechkv_shared_workspace_bytes(int32_t batch, int32_t num_groups, int32_
  *                cache_len[b] on are not written; those whose page is out of
  *                range keep their weight.
  * capacity       entries of a row of weights (>= 1).
- * Errors: INVALID_ARG, UNSUPPORTED (also where the launch would need 2^24
- *         blocks or more, or for caches of 2^31 - 8191 entries and more), HIP;
+ * Errors: INVALID_ARG, UNSUPPORTED (also where the launch would need 2^32
+ *         threads or more, or for caches of 2^31 - 8191 entries and more), HIP;
  *         ALIAS when weights_out overlaps anything read but for weights =
  *         weights_out.
  */

@@ -217,7 +217,9 @@ int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_ro
   a.batch = batch;
   a.cache = source_of(cache, cache_len, max_cache_len);
   plan_weights(a, n.dim * n.esz);
-  if (((__int128)batch * heads + 7) * a.key_blocks > kMaxBlocks) return SPEECHKV_ERR_UNSUPPORTED;
+  // (with many rows a block has 512 threads: 2^32 of a launch are too many)
+  if (((__int128)batch * heads + 7) * a.key_blocks > (a.row_tiles > kWeightFew ? kMaxBlocks / 2 : kMaxBlocks))
+    return SPEECHKV_ERR_UNSUPPORTED;
   const int64_t pool = page_pool_bytes(cache), lens = (int64_t)batch * 4, sums = rows_bytes(batch, heads, capacity);
   if (sums < 0) return SPEECHKV_ERR_INVALID_ARG;
   const Region rd[] = {{vq.p, vq.bytes}, {lse, lse_bytes}, {visible, lens * num_rows}, {cache_len, lens},
