@@ -363,7 +363,9 @@ constexpr int kFull = 8192;
 
 // A wave's step: about four rows a lane group, so that the angles are worked out
 // for several rows, but only while the steps fill the chip; with few of them the
-// waves share a step's rows.
+// waves share a step's rows, until they fill the chip eight times over (4095 tokens
+// of more than 136 heads of 128: behind it a lane group takes several rows, as a wave
+// for every eight could pass 2^32 threads of a launch).
 NormPart part_of(int tokens, int heads, int head_dim) {
   const int groups = 64 / (head_dim / 16);
   NormPart p;
@@ -376,7 +378,7 @@ NormPart part_of(int tokens, int heads, int head_dim) {
   if (!heads) return p;
   while (p.tokens < kNormTokens && p.tokens * heads < 4 * groups && tokens / (2 * p.tokens) >= kFull) p.tokens *= 2;
   p.steps = (tokens + p.tokens - 1) / p.tokens;
-  if (p.steps < kFull / 2) p.split = (p.tokens * heads + groups - 1) / groups;
+  if (p.steps < kFull / 2) p.split = std::min((p.tokens * heads + groups - 1) / groups, 1 + 8 * kFull / p.steps);
   p.blocks = (int)(((int64_t)p.steps * p.split + kThreads / 64 - 1) / (kThreads / 64));
   return p;
 }

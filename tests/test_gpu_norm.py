@@ -162,6 +162,24 @@ def test_in_place_and_beside_each_other():
         assert torch.equal(x.dq_out[b, :n], grads[0][b, :n]) and torch.equal(x.dk_out[b, :n], grads[1][b, :n])
 
 
+def test_more_heads_than_waves_share():
+    # a row gives the same bits in a call of all heads as in one of a few
+    S, H, D = 4095, 160, 128
+    q, dy = (inputs.normal((1, S, H, D), i, dtype=BF).to(DEV) for i in (1, 2))
+    gamma = (1 + 0.3 * inputs.normal((D,), 3, dtype=F32)).to(DEV)
+    rope = skv.Rope(torch.arange(S, dtype=torch.int32, device=DEV)[None],
+                    torch.logspace(0, -4, D // 2, dtype=F32, device=DEV))
+    out, dq, some, dsome = (torch.full_like(q, -7.0) for _ in range(4))
+    skv.speechkv_norm_rope(q, None, out, None, gamma_q=gamma, rope=rope)
+    skv.speechkv_norm_rope_bwd(q, None, dy, None, dq, None, gamma_q=gamma, rope=rope)
+    for h in range(0, H, 40):
+        at = (slice(None), slice(None), slice(h, h + 40))
+        skv.speechkv_norm_rope(q[at], None, some[at], None, gamma_q=gamma, rope=rope)
+        skv.speechkv_norm_rope_bwd(q[at], None, dy[at], None, dsome[at], None, gamma_q=gamma, rope=rope)
+    assert torch.equal(out, some) and torch.equal(dq, dsome)
+    assert bool((out[0, 0, :, 5] != -7.0).all())
+
+
 @pytest.mark.parametrize("which", ["q", "k"])
 def test_one_of_the_two(which):
     x = Inputs(4)
