@@ -216,7 +216,7 @@ int speechkv_attn_weights(const speechkv_heads* q, int32_t batch, int32_t num_ro
   a.row_tiles = (int)(((int64_t)num_rows * group + 15) / 16);
   a.batch = batch;
   a.cache = source_of(cache, cache_len, max_cache_len);
-  plan_weights(a, n.dim * n.esz);
+  plan_weights(a, n.dim, n.esz);
   // (with many rows a block has 512 threads: 2^32 of a launch are too many)
   if (((__int128)batch * heads + 7) * a.key_blocks > (a.row_tiles > kWeightFew ? kMaxBlocks / 2 : kMaxBlocks))
     return SPEECHKV_ERR_UNSUPPORTED;

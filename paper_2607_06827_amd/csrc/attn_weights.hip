@@ -13,14 +13,20 @@
 // Few rows (a decoding step): the rows stay in LDS and each wave streams keys of its
 // own, 32 a step, one step ahead.  Bound by reading the keys: 16 sequences of 7660 keys
 // of 8 heads take 46 us, 259 MB at 5.6 TB/s (reads alone reach 6.4).
-// Many rows (a prompt): a block holds 64 keys in its waves' registers, the waves deal
-// the row tiles out, each streaming those of its own, and add up through LDS.  8
-// prompts of 1596 tokens of 16 heads over 471 entries take 33 us, 360 TFLOP/s.  They are
-// bound by three things of like size that overlap in part: the rows' way into LDS (210
-// MB, a CU reads about 57 GB/s: 14 us), the products with their exponentials (16 us with
-// nothing to wait for), and the two rounds of blocks that load their keys first (the
-// kernel without its loop: 8 us).  Four waves a block, all blocks at once, took 46 us:
-// the first keys, which every row sees, set the time; six waves and two blocks a CU 38.
+// Many rows (a prompt): a block holds 64 keys in its waves' registers, or two
+// stretches of 64, the waves deal the row tiles out, each streaming those of its own,
+// and add up through LDS.  8 prompts of 1596 tokens of 16 heads over 471 entries take
+// 29.5 us, 400 TFLOP/s, with two stretches a block: the first and the last, the second
+// and the last but one and so on, so that all blocks are alike and one round of them
+// is enough (33.5 with one: two rounds that load their keys first, 8 us of them
+// without the loop, and 210 MB of rows into LDS for 152).  They are bound by what
+// overlaps in part: the rows' way into LDS (a CU reads about 57 GB/s: 10 us), the
+// products with their exponentials (16 us with nothing to wait for), the block's own
+// keys and its sums (5).  With two stretches a wave adds one row tile at a time: two
+// need more than 256 registers (60 us, as each key fragment read back from memory
+// waits for all loads); row addresses are scalar for the same reason (30.8).  Four
+// waves a block, all blocks at once, took 46 us: the first keys, which every row sees,
+// set the time; six waves and two blocks a CU 38.
 #include <algorithm>
 
 #include "kernels_shared.hpp"
@@ -32,6 +38,7 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;                  // few rows
 constexpr int kManyWaves = 8, kManyThreads = 64 * kManyWaves;  // many rows
+constexpr int kCus = 256;
 constexpr int kSpreadUnits = 32;  // pairs from which an XCD takes pairs of its own
 
 // Rows of 16-byte chunks in LDS: chunk c of row r at position c ^ swizzle(r).
@@ -329,28 +336,36 @@ __global__ __launch_bounds__(kThreads, 2) void weights_few_kernel(WeightArgs a) 
 
 // --------------------------------------------------------------- many rows
 
-template <typename T, int D>
+// kStretches: stretches of kKeys keys that a block holds, 1 or 2.  With two, block p has
+// stretch p and, of n, stretch n - 1 - p: in a prompt, where later keys have fewer
+// rows, all blocks have as many products, and the rows of the later are among those of
+// the earlier.
+template <typename T, int D, int kStretches>
 __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a) {
   typedef Rows16<T, D> L;
   constexpr int kKeys = weight_keys(L::kBytes), kTiles = kKeys / 16;
   constexpr int kAhead = L::kBytes > 256 ? 2 : 4;  // row tiles of a wave on their way
-  constexpr int kOnce = kAhead / 2;                // row tiles added at once
+  constexpr int kOnce = kStretches == 2 ? 1 : kAhead / 2;  // row tiles added at once
   constexpr int kN = L::kTileLoads + 1;            // direct loads of a row tile
   __shared__ __attribute__((aligned(1024))) unsigned char s_row[kManyWaves][kAhead][L::kTileBytes];
   __shared__ int s_info[kManyWaves][kAhead][64];  // lanes 0 .. 31: the rows' lse, 32 .. 63: what they see
-  __shared__ float s_part[kManyWaves][kKeys];
+  __shared__ float s_part[kManyWaves][kStretches * kKeys];
   __shared__ uint64_t s_sees[kManyWaves];
-  static_assert(sizeof(s_row) >= kTiles * L::kTileBytes, "the keys come through the rows' place");
+  static_assert(sizeof(s_row) >= kStretches * kTiles * L::kTileBytes, "the keys come through the rows' place");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   Unit u;
   if (!unit_of(a, u)) return;
-  const int kb = u.part * kKeys;
-  if (kb >= u.len) return;
+  const int kb = u.part * kKeys;  // first key of the first stretch
+  int kb2 = kb;                   // and of the second, the same if there is none
+  if constexpr (kStretches == 2) kb2 = ((u.len + kKeys - 1) / kKeys - 1 - u.part) * kKeys;
+  if (kb >= u.len || kb2 < kb) return;
 
-  float sum[4 * kTiles];
+  float sum[kStretches][4 * kTiles];
 #pragma unroll
-  for (int j = 0; j < 4 * kTiles; ++j) sum[j] = 0.f;
+  for (int c = 0; c < kStretches; ++c)
+#pragma unroll
+    for (int j = 0; j < 4 * kTiles; ++j) sum[c][j] = 0.f;
   const int queries = 16 >> a.group_shift, in = col >> a.group_shift;
 
   // kManyWaves * 64 row tiles at a time, 64 a wave: lane n finds out whether any row
@@ -371,39 +386,51 @@ __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a
   const int rt0_first = rt0;
   uint64_t sees;
 
-  u32x4_t k[kTiles][L::kPieces];
-  uint64_t present;  // keys that have a page
+  u32x4_t k[kStretches][kTiles][L::kPieces];
+  uint64_t present[kStretches];  // keys that have a page
   {
     const int32_t* table = a.cache.table + (int64_t)u.b * a.cache.pv.max_pages;
-    const int entry = table[min(kb + lane, u.len - 1) >> a.cache.pv.page_shift];
-    present = __builtin_amdgcn_ballot_w64(entry >= 0 && entry < a.cache.pv.num_pages);
+    int entry[kStretches];
+#pragma unroll
+    for (int c = 0; c < kStretches; ++c)
+      entry[c] = table[min((c ? kb2 : kb) + lane, u.len - 1) >> a.cache.pv.page_shift];
     const uint32_t sk = lds_addr(s_row);
-    load_keys<T, D, kTiles, 0, false>(a, u, kb, entry, 0, sk, lane, wave, kManyWaves);
+#pragma unroll
+    for (int c = 0; c < kStretches; ++c) {
+      present[c] = __builtin_amdgcn_ballot_w64(entry[c] >= 0 && entry[c] < a.cache.pv.num_pages);
+      load_keys<T, D, kTiles, 0, false>(a, u, c ? kb2 : kb, entry[c], 0, sk + c * kTiles * L::kTileBytes, lane, wave,
+                                        kManyWaves);
+    }
     sees = scan(rt0);  // (on its way with the keys)
     wait_vm<0>();
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) L::read(k[t], sk + t * L::kTileBytes, col, quarter);
+    for (int c = 0; c < kStretches; ++c)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) L::read(k[c][t], sk + (c * kTiles + t) * L::kTileBytes, col, quarter);
     wait_lds();
     __syncthreads();  // the keys are in registers: rows take their place
   }
 
   const uint32_t s_rows = lds_addr(s_row[wave]), s_infos = lds_addr(s_info[wave]);
-  // where this lane reads its share of a tile: in a tile whose queries are all there,
-  // as far behind tile 0's as the tile's first query behind query 0
-  const char* from[L::kTileLoads];
-#pragma unroll
-  for (int n = 0; n < L::kTileLoads; ++n) {
-    const int row = n * L::kPerLoad + lane / L::kChunks;
-    from[n] = row_of<T>(a, u, 0, row) + ((lane % L::kChunks ^ L::swizzle(row)) << 4);
-  }
+  // A lane reads chunk `lpos` (swizzled) of row `lrow` of each load.  Rows r = n
+  // kPerLoad + lrow of a tile have no carry between the two, neither in their query
+  // nor in their head: the first gives a scalar base, the second this lane's offset
+  // (where 32 bits hold it).
+  const int lrow = lane / L::kChunks, gmask = (1 << a.group_shift) - 1;
+  const int64_t lane_at = ((lrow >> a.group_shift) * a.q.ss + (lrow & gmask) * a.q.sh) * (int)sizeof(T);
+  const bool near = !__builtin_amdgcn_ballot_w64(lane_at > INT32_MAX);
+  const uint32_t lane_off = (uint32_t)lane_at, lane_chunk = (lane % L::kChunks ^ L::swizzle(lrow)) << 4;
   const int64_t row_step = queries * a.q.ss * (int)sizeof(T);
   auto request = [&](int rt, int buffer) __attribute__((always_inline)) {
-    if ((rt + 1) * queries <= a.num_rows) {
+    if (near && (rt + 1) * queries <= a.num_rows) {
 #pragma unroll
-      for (int n = 0; n < L::kTileLoads; ++n)
-        lds_dma16_from<false>(from[n] + rt * row_step,
-                              __builtin_amdgcn_readfirstlane(s_rows + buffer * L::kTileBytes + n * 1024));
+      for (int n = 0; n < L::kTileLoads; ++n) {
+        const int row = n * L::kPerLoad;  // (a constant)
+        const char* base = row_of<T>(a, u, 0, row) + rt * row_step;
+        lds_dma16(base, lane_off + (lane_chunk ^ (L::swizzle(row) << 4)),
+                  __builtin_amdgcn_readfirstlane(s_rows + buffer * L::kTileBytes + n * 1024));
+      }
     } else {
       load_rows<T, D>(a, u, rt, s_rows + buffer * L::kTileBytes, lane);
     }
@@ -437,7 +464,7 @@ __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a
         todo ^= (uint64_t)1 << bit;
         last = rt0 + 64 * word + bit;
       }
-      return last;
+      return __builtin_amdgcn_readfirstlane(last);
     };
     int tile[kAhead];
 #pragma unroll
@@ -456,19 +483,34 @@ __global__ __launch_bounds__(kManyThreads) void weights_many_kernel(WeightArgs a
         wait_lds();
 #pragma unroll
         for (int m = 0; m < kOnce; ++m) request(tile[j + m] = next(), j + m);  // (always: what waits counts on it)
-        if (at + j < count) add_rows<T, D, kTiles>(a, k, y, kb, quarter, sum);
+        if (at + j < count) {
+          add_rows<T, D, kTiles>(a, k[0], y, kb, quarter, sum[0]);
+          if constexpr (kStretches == 2) {
+            int most = y[0].seen;
+#pragma unroll
+            for (int m = 1; m < kOnce; ++m) most = max(most, y[m].seen);
+            if (__builtin_amdgcn_ballot_w64(most > kb2)) add_rows<T, D, kTiles>(a, k[1], y, kb2, quarter, sum[1]);
+          }
+        }
       }
     }
     wait_vm<0>();
   }
-  s_part[wave][key_of<kTiles>(col, quarter)] = transposed_sum(sum, lane);
-  __syncthreads();
-  if (tid < kKeys && kb + tid < u.len) {
-    float total = 0.f;
 #pragma unroll
-    for (int v = 0; v < kManyWaves; ++v) total += s_part[v][tid];
-    const int64_t to = (int64_t)u.pair * a.capacity + kb + tid;
-    a.weights_out[to] = (a.weights ? a.weights[to] : 0.f) + (present >> tid & 1 ? total : 0.f);
+  for (int c = 0; c < kStretches; ++c)
+    s_part[wave][c * kKeys + key_of<kTiles>(col, quarter)] = transposed_sum(sum[c], lane);
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < kStretches; ++c) {
+    if (c && kb2 == kb) break;
+    const int key = (c ? kb2 : kb) + tid;
+    if (tid < kKeys && key < u.len) {
+      float total = 0.f;
+#pragma unroll
+      for (int v = 0; v < kManyWaves; ++v) total += s_part[v][c * kKeys + tid];
+      const int64_t to = (int64_t)u.pair * a.capacity + key;
+      a.weights_out[to] = (a.weights ? a.weights[to] : 0.f) + (present[c] >> tid & 1 ? total : 0.f);
+    }
   }
 }
 
@@ -482,8 +524,9 @@ hipError_t launch_weights_d(const WeightArgs& args, hipStream_t s) {
   const bool spread = pairs >= kSpreadUnits;
   a.by_pairs = FastDivide((int32_t)(spread ? (pairs + 7) / 8 : pairs));  // (of an XCD)
   const dim3 grid((uint32_t)((spread ? (pairs + 7) / 8 * 8 : pairs) * a.key_blocks));
-  return a.row_tiles > kWeightFew ? launch_struct(weights_many_kernel<T, D>, grid, dim3(kManyThreads), s, a)
-                                  : launch_struct(weights_few_kernel<T, D>, grid, dim3(kThreads), s, a);
+  if (a.row_tiles <= kWeightFew) return launch_struct(weights_few_kernel<T, D>, grid, dim3(kThreads), s, a);
+  return a.stretches == 2 ? launch_struct(weights_many_kernel<T, D, 2>, grid, dim3(kManyThreads), s, a)
+                          : launch_struct(weights_many_kernel<T, D, 1>, grid, dim3(kManyThreads), s, a);
 }
 
 hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStream_t s) {
@@ -491,13 +534,30 @@ hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStrea
   return head_dim == 128 ? launch_weights_d<float, 128>(a, s) : launch_weights_d<float, 64>(a, s);
 }
 
-// Steps of a wave with few rows: what spreads the keys over the blocks that run at
-// once (two a CU), so that they end together.
-void plan_weights(WeightArgs& a, int row_bytes) {
+// Many rows: one or two stretches of keys a block, what an estimate says is faster.
+// A CU holds one block at a time, which takes 5 us and 0.105 for a row tile and
+// stretch (128-wide bf16 heads; 0.07 with 64-wide ones, 0.37 in fp32).  As many rows
+// see a stretch as in a prompt: single ones, the largest first, end together but for
+// half of the last, pairs are all alike.  (8 sequences of 471 entries, 1596 rows: 36
+// us with one, 32 with two; of 300 entries, where pairs are 192 blocks, 27 and 33.)
+static int stretches_of(int64_t pairs, int64_t all, int row_tiles, int dim, int elt_size) {
+  const double block = 5.0, rows = row_tiles * (elt_size == 4 ? 0.37 : dim == 128 ? 0.105 : 0.07);
+  const double n = (double)pairs * all, tail = n > kCus ? 0.5 * (block + rows / all) : 0.0;
+  const double one = std::max(block + rows, (n * block + rows * pairs * (all + 1) / 2) / kCus + tail);
+  const double rounds = (double)((pairs * ((all + 1) / 2) + kCus - 1) / kCus);
+  return rounds * (1.1 * block + rows * (1.0 + 1.0 / all)) < one ? 2 : 1;
+}
+
+// Few rows: steps of a wave that spread the keys over the blocks that run at once (two
+// a CU), so that they end together.
+void plan_weights(WeightArgs& a, int dim, int elt_size) {
+  const int row_bytes = dim * elt_size;
   const int64_t pairs = (int64_t)a.batch * a.cache.pv.kv_heads;
   if (a.row_tiles > kWeightFew) {
+    const int64_t all = ((int64_t)a.cache.max_len + weight_keys(row_bytes) - 1) / weight_keys(row_bytes);
     a.steps = 1;
-    a.key_blocks = (int)(((int64_t)a.cache.max_len + weight_keys(row_bytes) - 1) / weight_keys(row_bytes));
+    a.stretches = all > 1 ? stretches_of(pairs, all, a.row_tiles, dim, elt_size) : 1;
+    a.key_blocks = (int)((all + a.stretches - 1) / a.stretches);
     return;
   }
   const int64_t tiles = ((int64_t)a.cache.max_len + kWeightStep - 1) / kWeightStep;

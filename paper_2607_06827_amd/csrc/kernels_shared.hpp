@@ -50,6 +50,7 @@ struct WeightArgs {
   int capacity;
   int row_tiles;   // tiles of 16 rows of a (sequence, KV head)
   int steps;       // with few rows: steps of a wave (set by the plan, as key_blocks)
+  int stretches;   // with many rows: stretches of keys of a block (as steps)
   int key_blocks;  // blocks of a (sequence, KV head)
   FastDivide by_pairs, by_heads;  // (set by the launcher)
 };
@@ -58,7 +59,7 @@ constexpr int kWeightStep = 32;   // keys of a wave's step with few rows
 constexpr int kWeightSteps = 16;  // most steps of a wave
 // Keys of a block with many rows.
 constexpr int weight_keys(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
-void plan_weights(WeightArgs& a, int row_bytes);
+void plan_weights(WeightArgs& a, int dim, int elt_size);
 
 // Layers of one launch of the eviction's kernels: their descriptions travel as
 // kernel arguments (4 KB at most).

@@ -232,6 +232,14 @@ WEIGHTS = [
     (BF, 64, 8, 8, 16, [9000, 4001, 17], 1, "last"),  # several steps of keys a wave
     (BF, 64, 8, 1, 16, [90], 1100, "any"),  # more row tiles than are looked through at once
     (F32, 128, 8, 1, 16, [70], 1030, "last"),
+    # two stretches of keys a block: one, two and more of them in a sequence, odd and even
+    (BF, 128, 8, 8, 16, [130, 64, 65, 0, 192, 193, 256, 257, 1, 70, 120], 37, "any"),
+    (BF, 64, 32, 32, 8, [300, 129, 63], 40, "last"),
+    (F32, 128, 16, 16, 32, [100, 33, 32, 161, 7], 35, "any"),
+    (F32, 64, 64, 32, 16, [310, 1, 128], 20, "last"),
+    (BF, 128, 16, 16, 16, [500, 449, 385, 70], 35, "last"),
+    (BF, 128, 32, 16, 64, [450, 65, 512, 1], 18, "any"),
+    (F32, 64, 32, 32, 16, [510, 300], 36, "any"),
 ]
 
 
@@ -543,6 +551,21 @@ def test_offsets_past_32_bits():
     skv.speechkv_norm_rope_bwd(rows, None, want, None, dx, None)
     skv.speechkv_norm_rope(rows, None, rows, None)
     assert torch.equal(rows, want) and torch.equal(dx, dwant)
+
+
+def test_weights_of_heads_that_lie_far_apart():
+    # heads 1.4 GB apart: the rows of one load span more than 31 bits
+    Hq, Hkv, D, S, L = 4, 1, 128, 40, 300
+    apart = 7 * 10 ** 8
+    cache = make_cache(1, L, Hkv, D, BF, 16, seed=90)
+    q = inputs.normal((1, S, Hq, D), 91, dtype=BF).to(DEV)
+    far = torch.as_strided(torch.empty(3 * apart + S * D, dtype=BF, device=DEV), (1, S, Hq, D), (0, D, apart, 1))
+    far.copy_(q)
+    lse = torch.full((1, Hq, S), 3.0, device=DEV)
+    one, two = (torch.full((1, Hkv, L), -1.0, device=DEV) for _ in range(2))
+    skv.speechkv_attn_weights(q, lse, cache, i32([L]), L, one)
+    skv.speechkv_attn_weights(far, lse, cache, i32([L]), L, two)
+    assert torch.equal(one, two) and bool((one >= 0).all())
 
 
 # ------------------------------------------------------------- all together
