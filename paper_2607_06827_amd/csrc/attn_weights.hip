@@ -16,7 +16,7 @@
 // Many rows (a prompt): a block holds 64 keys in its waves' registers, or two
 // stretches of 64, the waves deal the row tiles out, each streaming those of its own,
 // and add up through LDS.  8 prompts of 1596 tokens of 16 heads over 471 entries take
-// 29.5 us, 400 TFLOP/s, with two stretches a block: the first and the last, the second
+// 28 to 30 us, 400 TFLOP/s, with two stretches a block: the first and the last, the second
 // and the last but one and so on, so that all blocks are alike and one round of them
 // is enough (33.5 with one: two rounds that load their keys first, 8 us of them
 // without the loop, and 210 MB of rows into LDS for 152).  They are bound by what

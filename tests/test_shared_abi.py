@@ -159,15 +159,15 @@ def test_weights_rejects_overlaps(kw):
     assert weights(**kw) == E_ALIAS
 
 
+@NO_GPU
 def test_weights_refuse_launches_of_two_to_the_32_threads():
-    # 65535 sequences of 128 heads: a block of 512 threads for every 64 keys with many
-    # rows, of 256 threads for more keys with few
-    big = dict(c=cache(num_kv_heads=128, num_pages=1), q=heads(8, h=128, sb=0, ss=0, sh=64), batch=65535, lse=at(9), lb=0,
-               lh=0, ls=0, visible=None, capacity=128, w=None, out=at(10 ** 6))
-    assert weights(**{**big, "rows": 64, "max_len": 65}) == E_UNS
-    if not torch.cuda.is_available():
-        assert weights(**{**big, "rows": 64, "max_len": 64}) == E_HIP
-        assert weights(**{**big, "rows": 1, "max_len": 65}) == E_HIP
+    # 65535 sequences of 128 heads: a block of 512 threads for every 128 keys at most with
+    # many rows, of 256 threads for more keys with few
+    big = dict(c=cache(num_kv_heads=128, num_pages=1, max_pages_per_seq=20), q=heads(8, h=128, sb=0, ss=0, sh=64), batch=65535,
+               lse=at(9), lb=0, lh=0, ls=0, visible=None, capacity=200, w=None, out=at(10 ** 6))
+    assert weights(**{**big, "rows": 64, "max_len": 129}) == E_UNS
+    assert weights(**{**big, "rows": 64, "max_len": 64}) == E_HIP
+    assert weights(**{**big, "rows": 1, "max_len": 129}) == E_HIP
 
 
 @NO_GPU
