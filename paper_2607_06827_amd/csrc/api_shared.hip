@@ -33,12 +33,16 @@ size_t shared_bytes(int32_t batch, int32_t q_heads, int32_t head_dim, const Shar
 // The estimate is fitted to a sweep on MI355X over 20 shapes of 1 to 64 sequences
 // in 1 to 20 groups, 1 to 8 KV heads of 1 to 8 query heads, prefixes of 126 to 7532
 // and own caches of 10 to 5000 entries, both element types and head sizes; its
-// choice takes 1.8% longer than the best of the candidates on average, 9% at most.
+// choice takes 0.7% longer than the best of the candidates on average, 4.4% at most.
 // In us:
 //  - a block takes 0.3, a step of its four waves over a 128-wide bf16 tile each 1.21,
 //    one of a wave with own entries 1.37; 64-wide heads take 0.58 of it, fp32 5.1 and
 //    2.3 times; what runs at once is two blocks a CU (four with 64-wide bf16 heads, one
 //    with 128-wide fp32), and a full chip takes 1.5 times as long as its blocks alone;
+//  - the blocks that a CU has at first (numbers 0, 256, .. of the launch) take 0.8 of
+//    what they take one after the other (1.8% and 9% without this and the next);
+//  - (group, KV head, split)s go round the eight XCDs, so the fullest XCD counts for
+//    all (1.3% and 12% without this);
 //  - keys are read at 6.5 TB/s, once;
 //  - each partial row is written and read at 2.3 TB/s.
 SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_heads, int head_dim, int dtype,
@@ -49,7 +53,8 @@ SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_h
   const double units = (double)groups * kv_heads, own_units = (double)batch * kv_heads;
   const double row_tiles = std::ceil(members * group / kSharedRows), row_bytes = head_dim * (f32 ? 4.0 : 2.0);
   const int64_t tiles = std::max<int64_t>(1, tiles_of(max_prefix)), own = std::max<int64_t>(1, tiles_of(max_len));
-  const double slots = 256.0 * (f32 && wide ? 1 : !f32 && !wide ? 4 : 2);
+  const int per_cu = f32 && wide ? 1 : !f32 && !wide ? 4 : 2;
+  const double slots = 256.0 * per_cu;
   const double size = f32 ? (wide ? 5.08 : 2.29) : wide ? 1.0 : 0.58;
   const double read_us = (units * max_prefix + own_units * max_len) * 2 * row_bytes / 6.5e6;
   static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
@@ -62,8 +67,12 @@ SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_h
     for (int o : counts) {
       if (o > own || o > 32) break;
       const double own_us = 0.31 + 1.37 * size * (double)((own + o - 1) / o);
-      const double all_us = 1.5 * (units * row_tiles * s * block_us + std::ceil(own_units * o / 4) * own_us) / slots;
-      const double us = std::max({block_us, own_us, all_us, 0.31 + read_us}) +
+      const double blocks = std::ceil(units * s / 8) * 8 * row_tiles, own_blocks = std::ceil(own_units * o / 4);
+      const double all_us = 1.5 * (blocks * block_us + own_blocks * own_us) / slots;
+      double cu_us = 0.0;
+      for (int k = 0; k < per_cu && 256.0 * k < blocks + own_blocks; ++k)
+        cu_us += 0.8 * (256.0 * k < blocks ? block_us : own_us);
+      const double us = std::max({block_us, own_us, all_us, cu_us, 0.31 + read_us}) +
                         own_units * group * (s + o) * head_dim * 8 / 2.34e6;
       if (us < best_us) {
         best_us = us;
