@@ -17,13 +17,14 @@
 // the next K requested as soon as S^T is there, the next V as soon as O^T is: no
 // barrier.  More than 32 rows are more blocks that read the same keys, side by side
 // on one XCD and out of its L2 (on different XCDs HBM gives the keys to each: 64
-// questions about 7532 entries 24 us, 21 so).  There the kernel takes 18.8 us and the
+// questions about 7532 entries 24 us, 21 so).  There the kernel takes 17 us and the
 // merge 4: a CU reads about 57 GB/s whatever is on its way, and four row tiles bring
 // 123 MB into LDS; more splits or fewer rows a block cost partial rows or reads.  Six
 // recordings of 1532 entries with 40 questions of up to 301 own ones take 17.6 and 4
 // us, 59 MB.  Blocks of 64 or 128 rows, whose waves
 // share a tile and a barrier, are slower (23 and 25 us), also with four tiles on their
-// way, and so are blocks of eight waves.
+// way, and so are blocks of eight waves, and waves with 64 rows each (one block a CU
+// for their 297 registers: 24 us).
 //
 // Every row of a block sees the same keys, so keys that are not there (past the
 // last, or without a page) are masked for all: their logits become -inf and their
