@@ -163,12 +163,14 @@ __device__ __forceinline__ const char* row_of(const WeightArgs& a, const Unit& u
                                        h * a.q.sh);
 }
 
-// Direct loads of row tile rt into LDS at `to`, by one wave.
+// Direct loads of row tile rt into LDS at `to`, by one wave.  (One after the other: the
+// last tile takes this way, and four loads' addresses would take the registers of
+// keys.)
 template <typename T, int D>
 __device__ __forceinline__ void load_rows(const WeightArgs& a, const Unit& u, int rt, uint32_t to, int lane) {
   typedef Rows16<T, D> L;
   const int lrow = lane / L::kChunks, lpos = lane % L::kChunks;
-#pragma unroll
+#pragma nounroll
   for (int n = 0; n < L::kTileLoads; ++n) {
     const int row = n * L::kPerLoad + lrow;
     lds_dma16_from<false>(row_of<T>(a, u, rt, row) + ((lpos ^ L::swizzle(row)) << 4),
