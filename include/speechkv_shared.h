@@ -63,13 +63,18 @@ extern "C" {
  * max_cache_len  host bound on cache_len.
  * scale          logit scale, finite and > 0.
  * num_splits     key ranges that a prefix is split into, 1 .. 1024; 0 selects
- *                speechkv_shared_num_splits().  Partial results are merged in a
- *                fixed order: the same call gives the same bits.
+ *                speechkv_shared_num_splits(), or the best count that the
+ *                workspace holds.  Partial results are merged in a fixed order:
+ *                the same call, with a workspace of the same size, gives the
+ *                same bits.
  * lse            device fp32 [batch][num_q_heads] receiving the natural-log
  *                log-sum-exp of each row's scaled logits (-inf where it sees
  *                nothing), or NULL.
- * workspace      device scratch, 16-byte aligned, of at least
- *                speechkv_shared_workspace_bytes(...) bytes; any contents.
+ * workspace      device scratch, 16-byte aligned; any contents.  With num_splits
+ *                = 0 any size from batch * num_q_heads * (head_dim + 2) * 8 bytes
+ *                on does; a call that has less than
+ *                speechkv_shared_workspace_bytes(...) takes fewer splits, which
+ *                may be slower.  With a given count it must hold that size.
  *                Calls that overlap in time need one each.
  * Errors: INVALID_ARG, WORKSPACE, HIP; UNSUPPORTED also where a launch would
  *         need 2^24 blocks or more, or for caches of 2^31 - 8191 entries and
@@ -84,9 +89,12 @@ int speechkv_shared_attn(const void* q, int32_t batch, int32_t num_q_heads,
                          int32_t max_cache_len, float scale, int32_t num_splits, void* out,
                          float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* The split count speechkv_shared_attn takes for num_splits = 0 (-1 for invalid
- * arguments), and the workspace it needs for num_splits (0: for its own choice
- * with either element type; the size 0 stands for invalid arguments).  Host
+/* The split count speechkv_shared_attn takes for num_splits = 0 with workspace
+ * enough (-1 for invalid arguments), and the workspace it needs for num_splits
+ * (0: enough for its own choice with either element type; the size 0 stands for
+ * invalid arguments).  The choice falls where more members or entries fill the
+ * chip, so a larger call may need less: a program whose calls vary asks for
+ * every one of them, or keeps the largest size that it is ready to spend.  Host
  * only. */
 int32_t speechkv_shared_num_splits(int32_t batch, int32_t num_groups, int32_t max_group,
                                    int32_t num_q_heads, int32_t num_kv_heads,

@@ -28,8 +28,10 @@ size_t shared_bytes(int32_t batch, int32_t q_heads, int32_t head_dim, const Shar
   return (size_t)batch * q_heads * (p.splits + p.own_splits) * (head_dim + 2) * sizeof(float);
 }
 
-// The plan with the smallest estimated time (with the given prefix splits, or of its
-// own choice).
+// The plan with the smallest estimated time: with the given prefix splits, or with 0 of
+// those whose partial rows fit `room` bytes (or the smallest of all).  (The best counts
+// fall where more members or entries fill the chip, so room for the largest call may be
+// too little for a smaller one's.)
 // The estimate is fitted to a sweep on MI355X over 20 shapes of 1 to 64 sequences
 // in 1 to 20 groups, 1 to 8 KV heads of 1 to 8 query heads, prefixes of 126 to 7532
 // and own caches of 10 to 5000 entries, both element types and head sizes; its
@@ -46,7 +48,7 @@ size_t shared_bytes(int32_t batch, int32_t q_heads, int32_t head_dim, const Shar
 //  - keys are read at 6.5 TB/s, once;
 //  - each partial row is written and read at 2.3 TB/s.
 SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_heads, int head_dim, int dtype,
-                       int max_prefix, int max_len, int splits) {
+                       int max_prefix, int max_len, int splits, size_t room) {
   const bool f32 = dtype == SPEECHKV_DTYPE_F32, wide = head_dim == 128;
   // members of a group: between the average and the bound
   const double members = 0.5 * (max_group + std::min<double>(max_group, (double)batch / groups));
@@ -66,6 +68,7 @@ SharedPlan shared_plan(int batch, int groups, int max_group, int group, int kv_h
     const double block_us = 0.31 + 1.21 * size * (double)(((tiles + s - 1) / s + 3) / 4);
     for (int o : counts) {
       if (o > own || o > 32) break;
+      if (!splits && shared_bytes(batch, group * kv_heads, head_dim, {s, o}) > room) break;
       const double own_us = 0.31 + 1.37 * size * (double)((own + o - 1) / o);
       const double blocks = std::ceil(units * s / 8) * 8 * row_tiles, own_blocks = std::ceil(own_units * o / 4);
       const double all_us = 1.5 * (blocks * block_us + own_blocks * own_us) / slots;
@@ -116,7 +119,7 @@ int32_t speechkv_shared_num_splits(int32_t batch, int32_t num_groups, int32_t ma
   const int group = group_of(num_q_heads, num_kv_heads);
   if (group < 0) return -1;
   return shared_plan(batch, num_groups, max_group, group, num_kv_heads, head_dim, dtype, max_prefix_len, max_cache_len,
-                     0)
+                     0, SIZE_MAX)
       .splits;
 }
 
@@ -131,7 +134,7 @@ size_t speechkv_shared_workspace_bytes(int32_t batch, int32_t num_groups, int32_
   for (int dtype : {SPEECHKV_DTYPE_F32, SPEECHKV_DTYPE_BF16})
     most = std::max(most, shared_bytes(batch, num_q_heads, head_dim,
                                        shared_plan(batch, num_groups, max_group, num_q_heads / num_kv_heads, num_kv_heads,
-                                                   head_dim, dtype, max_prefix_len, max_cache_len, num_splits)));
+                                                   head_dim, dtype, max_prefix_len, max_cache_len, num_splits, SIZE_MAX)));
   return most;
 }
 
@@ -156,7 +159,7 @@ int speechkv_shared_attn(const void* q, int32_t batch, int32_t num_q_heads, cons
       !aligned4(cache_len))
     return SPEECHKV_ERR_INVALID_ARG;
   const SharedPlan plan = shared_plan(batch, num_groups, max_group, group, heads, D, cache->dtype, max_prefix_len,
-                                      max_cache_len, num_splits);
+                                      max_cache_len, num_splits, workspace ? workspace_bytes : 0);
   const size_t need = shared_bytes(batch, num_q_heads, D, plan);
   if (!workspace || workspace_bytes < need || !aligned16(workspace)) return SPEECHKV_ERR_WORKSPACE;
   const int row_tiles = row_tiles_of((int64_t)max_group * group);

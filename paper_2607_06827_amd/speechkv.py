@@ -1039,8 +1039,9 @@ def speechkv_shared_attn(q: torch.Tensor, prefix: PagedKV, prefix_len: torch.Ten
     """q, out: [B, Hq, D] contiguous; prefix: the prefixes' cache, a row of its
     block table a group; prefix_len: int32 [groups]; group_start: int32 [groups
     + 1]; cache, cache_len: the sequences' own entries, int32 [B]; lse: fp32
-    [B, Hq] or None; workspace: device bytes, at least
-    speechkv_shared_workspace_bytes(...)."""
+    [B, Hq] or None; workspace: device bytes, speechkv_shared_workspace_bytes(...)
+    of them; with num_splits = 0 any size from B * Hq * (D + 2) * 8 on does (too
+    few: fewer splits)."""
     shape, dt, dev = q.shape, q.dtype, q.get_device()
     if len(shape) != 3 or out.shape != shape or not q.is_contiguous() or not out.is_contiguous():
         raise ValueError("q and out must be contiguous [B, Hq, D] tensors of one shape")
