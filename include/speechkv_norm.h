@@ -137,7 +137,8 @@ int speechkv_norm_rope_bwd(const speechkv_heads* q, const speechkv_heads* k,
 
 /* Workspace bytes of speechkv_norm_rope_bwd with a dgamma (num_q_heads or
  * num_kv_heads 0: without the queries or the keys), or 0 for invalid or
- * unsupported arguments.  Host only. */
+ * unsupported arguments.  The size for the most sequences and rows of a program
+ * is enough for fewer.  Host only. */
 size_t speechkv_norm_rope_bwd_workspace_bytes(int32_t batch, int32_t num_rows,
                                               int32_t num_q_heads, int32_t num_kv_heads,
                                               int32_t head_dim);

@@ -60,7 +60,7 @@ struct NormArgs {
 hipError_t launch_norm(const NormArgs& a, bool append, int dtype, int head_dim, hipStream_t s);
 // The backward, and with a.partial the sums of dgamma behind it.
 hipError_t launch_norm_bwd(const NormArgs& a, int dtype, int head_dim, hipStream_t s);
-// Blocks of the backward that write sums of dgamma.
+// Most blocks that write sums of dgamma in any backward of up to so many tokens.
 int norm_bwd_blocks(int tokens, int q_heads, int k_heads, int head_dim);
 
 }  // namespace skv
