@@ -98,8 +98,9 @@ typedef struct speechkv_rope {
  *                is; num_heads as in the input.  An output may be its own input
  *                (one address and one set of strides).
  * Errors: INVALID_ARG, UNSUPPORTED, HIP; ALIAS when an output overlaps anything
- *         read or the other output (but for its own input as above, and views
- *         of one tensor whose rows lie beside each other).
+ *         read or the other output (but for its own input as above, and heads
+ *         of one tensor, in any order of its axes, that lie beside each
+ *         other).
  */
 int speechkv_norm_rope(const speechkv_heads* q, const speechkv_heads* k, int32_t batch,
                        int32_t num_rows, const int32_t* row_len, int32_t head_dim,

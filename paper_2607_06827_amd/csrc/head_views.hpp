@@ -59,17 +59,33 @@ inline bool same(const View& a, const View& b, const Sizes& n) {
          (a.heads == 1 || a.sh == b.sh);
 }
 
-// Views whose byte ranges meet but whose rows do not: the heads of each row of b
-// lie behind those of the same row of a, before a's next row.
+// Views whose byte ranges meet but whose rows do not.  Both go in the same steps along
+// some of the outer axes (sequences, rows, or both), and of each such step b's part (the
+// axes that are left, and the heads) lies behind a's, before a's next: heads of one
+// projection's output in any order of its axes.
 inline bool beside(const View& a, const View& b, const Sizes& n) {
-  if ((n.batch > 1 && a.sb != b.sb) || (n.rows > 1 && a.ss != b.ss)) return false;
   const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
   if (off < 0 || off % n.esz) return false;
-  const int64_t d = off / n.esz, span_a = (a.heads - 1) * a.sh + n.dim, span_b = (b.heads - 1) * b.sh + n.dim;
-  const int64_t row = d + span_b;  // what a row of both takes
-  if (d < span_a) return false;
-  if (n.rows > 1 && row > a.ss) return false;
-  return n.batch == 1 || (n.rows > 1 ? (n.rows - 1) * a.ss : 0) + row <= a.sb;
+  const int64_t d = off / n.esz;
+  for (const auto& [by_batch, by_rows] : {std::pair(true, true), std::pair(true, false), std::pair(false, true)}) {
+    if ((by_batch && n.batch > 1 && a.sb != b.sb) || (by_rows && n.rows > 1 && a.ss != b.ss)) continue;
+    auto part = [&](const View& v) {
+      return (v.heads - 1) * v.sh + n.dim + (by_batch ? 0 : (n.batch - 1) * v.sb) + (by_rows ? 0 : (n.rows - 1) * v.ss);
+    };
+    if (d < part(a)) continue;
+    // (the steps nested, as those of a written view)
+    std::pair<int64_t, int32_t> axis[2] = {{a.sb, by_batch ? n.batch : 1}, {a.ss, by_rows ? n.rows : 1}};
+    std::sort(axis, axis + 2);
+    int64_t span = d + part(b);  // what a step of both takes
+    bool nested = true;
+    for (const auto& [stride, length] : axis) {
+      if (length == 1) continue;
+      nested = nested && stride >= span;
+      span += stride * (length - 1);
+    }
+    if (nested) return true;
+  }
+  return false;
 }
 
 inline bool clash(const View& a, const View& b, const Sizes& n) {
