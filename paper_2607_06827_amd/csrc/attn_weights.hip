@@ -256,8 +256,11 @@ __device__ __forceinline__ int key_of(int col, int quarter) {
 
 // ---------------------------------------------------------------- few rows
 
+// Blocks that run at once on a CU: fp32 rows of 128 elements take 152 KB of LDS a block.
+constexpr int few_blocks(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
+
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void weights_few_kernel(WeightArgs a) {
+__global__ __launch_bounds__(kThreads, few_blocks(Rows16<T, D>::kBytes)) void weights_few_kernel(WeightArgs a) {
   typedef Rows16<T, D> L;
   constexpr int kTiles = kWeightStep / 16, kStepBytes = kTiles * L::kTileBytes, kN = kTiles * L::kTileLoads;
   __shared__ __attribute__((aligned(1024))) unsigned char s_q[kWeightFew * L::kTileBytes];
@@ -550,8 +553,13 @@ static int stretches_of(int64_t pairs, int64_t all, int row_tiles, int dim, int 
   return rounds * (1.1 * block + rows * (1.0 + 1.0 / all)) < one ? 2 : 1;
 }
 
-// Few rows: steps of a wave that spread the keys over the blocks that run at once (two
-// a CU), so that they end together.
+// Few rows: steps of a wave that spread the keys over the blocks that run at once, so
+// that they end together.  (Cut for two blocks a CU where one fits, 4 sequences of 7660
+// keys of 8 heads in fp32 took 36 us for 30 and one took 17 for 13.)  Where that is more
+// steps than a wave has, one block a CU goes in whole rounds (9 of them 62 us, 77 with 16
+// steps a wave); two a CU overlap, and whole rounds are as often slower (20 sequences of
+// 64-wide bf16 keys 28 us with 16 steps and 33 in rounds, 34 of 4000 128-wide ones 63
+// and 58).
 void plan_weights(WeightArgs& a, int dim, int elt_size) {
   const int row_bytes = dim * elt_size;
   const int64_t pairs = (int64_t)a.batch * a.cache.pv.kv_heads;
@@ -563,8 +571,10 @@ void plan_weights(WeightArgs& a, int dim, int elt_size) {
     return;
   }
   const int64_t tiles = ((int64_t)a.cache.max_len + kWeightStep - 1) / kWeightStep;
-  const int64_t want = (pairs * tiles + 512 * kWaves - 1) / (512 * kWaves);
-  a.steps = (int)std::max<int64_t>(1, std::min<int64_t>(want, kWeightSteps));
+  const int64_t waves = (int64_t)kCus * few_blocks(row_bytes) * kWaves, all = pairs * tiles;
+  const int64_t rounds =
+      few_blocks(row_bytes) > 1 ? 1 : std::max<int64_t>(1, (all + waves * kWeightSteps - 1) / (waves * kWeightSteps));
+  a.steps = (int)std::max<int64_t>(1, std::min<int64_t>((all + waves * rounds - 1) / (waves * rounds), kWeightSteps));
   a.key_blocks = (int)((tiles + kWaves * a.steps - 1) / (kWaves * a.steps));
 }
 

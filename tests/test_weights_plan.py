@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2607_06827_amd import speechkv as skv
+from test_kernel_resources import kernels
 from test_sanitizers import HIPCC, PKG
 from weights_cases import BF, TWO_STRETCHES, requested_ahead, row_tiles
 
@@ -56,3 +57,24 @@ def test_the_cases_of_two_stretches_take_two(plan):
         assert stretches == 2 and blocks == -(-max(c[5]) // (2 * keys)), c
         assert row_tiles(c) > requested_ahead(c), c
     assert any(row_tiles(c) % 8 for c in TWO_STRETCHES) and sum(row_tiles(c) > 512 for c in TWO_STRETCHES) >= 2
+
+
+# bf16 and fp32 rows of 64 and 128 elements: the kernel's name in the library
+FEW = {(64, 2): "weights_few_kernelItLi64E", (128, 2): "weights_few_kernelItLi128E",
+       (64, 4): "weights_few_kernelIfLi64E", (128, 4): "weights_few_kernelIfLi128E"}
+CUS, LDS = 256, 160 * 1024
+
+
+@pytest.mark.parametrize("dim,esz", list(FEW))
+def test_few_rows_spread_over_the_blocks_that_run_at_once(plan, dim, esz):
+    """A wave's steps cut the keys for one round of blocks, of as many as a CU's LDS
+    holds, or, one a CU, for as few whole rounds as it takes."""
+    found = [k for n, k in kernels().items() if FEW[dim, esz] in n]
+    assert len(found) == 1
+    at_once = CUS * min(LDS // found[0][".group_segment_fixed_size"], 2)
+    calls = [(B, H, L, 1, dim, esz) for B in (1, 2, 3, 8, 16, 40) for H in (1, 4, 8) for L in (1, 31, 471, 1600, 7660, 60000)]
+    for (B, H, L, *_), (steps, _, blocks) in zip(calls, plan(calls)):
+        tiles = -(-L // 32)
+        rounds = -(-B * H * tiles // (at_once * 4 * 16)) if at_once == CUS else 1  # of 16 steps a wave at most
+        assert 1 <= steps <= 16 and blocks == -(-tiles // (4 * steps))
+        assert steps == min(-(-B * H * tiles // (at_once * 4 * rounds)), 16), (B, H, L, steps, rounds)
