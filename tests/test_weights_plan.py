@@ -6,8 +6,8 @@ import subprocess
 import pytest
 
 from paper_2607_06827_amd import speechkv as skv
+from paper_2607_06827_amd.build import CSRC, HIPCC
 from test_kernel_resources import kernels
-from test_sanitizers import HIPCC, PKG
 from weights_cases import BF, TWO_STRETCHES, requested_ahead, row_tiles
 
 CLIENT = r"""
@@ -38,7 +38,7 @@ def plan(tmp_path_factory):
     at = tmp_path_factory.mktemp("plan")
     (at / "plan.hip").write_text(CLIENT)
     lib = os.path.dirname(skv.LIBRARY_PATH)
-    subprocess.run([HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", f"-I{os.path.join(PKG, 'csrc')}",
+    subprocess.run([HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", f"-I{CSRC}",
                     str(at / "plan.hip"), "-o", str(at / "plan"), f"-L{lib}", "-lspeechkv", f"-Wl,-rpath,{lib}"], check=True,
                    capture_output=True)
 
