@@ -116,7 +116,9 @@ size_t speechkv_shared_workspace_bytes(int32_t batch, int32_t num_groups, int32_
  * Each row sees a prefix of the cache: its first visible[b][i] entries.  With
  * the lse of an attention over those entries a row gives 1 in all; with that of
  * speechkv_shared_attn it gives 1 in all to the prefix and the own entries
- * together.  A row whose lse is -inf (one that sees nothing) gives nothing.
+ * together.  The lse of a prompt is speechkv_prefill_attn's, that of a decoding
+ * step speechkv_shared_attn's (with one empty group where nothing is shared):
+ * speechkv_decode_attn and speechkv_tree_attn return none.  A row whose lse is -inf (one that sees nothing) gives nothing.
  * Products and sums are fp32.
  *
  * q              host pointer to the queries' description (batch, num_rows,

@@ -12,14 +12,17 @@
 //
 // Few rows (a decoding step): the rows stay in LDS and each wave streams keys of its
 // own, 32 a step, one step ahead.  Bound by reading the keys: 16 sequences of 7660 keys
-// of 8 heads take 46 us, 259 MB at 5.6 TB/s (reads alone reach 6.4).
+// of 8 heads take 46 us, 259 MB at 5.6 TB/s (reads alone reach 6.4); in fp32, one block
+// a CU, 103 us, 510 MB at 5.0, and 4 of them 31, 4.1.
 // Many rows (a prompt): a block holds 64 keys in its waves' registers, or two
 // stretches of 64, the waves deal the row tiles out, each streaming those of its own,
 // and add up through LDS.  8 prompts of 1596 tokens of 16 heads over 471 entries take
 // 28 to 30 us, 400 TFLOP/s, with two stretches a block: the first and the last, the second
 // and the last but one and so on, so that all blocks are alike and one round of them
-// is enough (33.5 with one: two rounds that load their keys first, 8 us of them
-// without the loop, and 210 MB of rows into LDS for 152).  They are bound by what
+// is enough (34 with one: two rounds that load their keys first, 8 us of them
+// without the loop, and 210 MB of rows into LDS for 152).  Nothing splits the rows of a
+// stretch: few (sequence, KV head)s leave CUs idle beside the blocks of the first keys,
+// and one or two of these prompts take 24 us as well.  They are bound by what
 // overlaps in part: the rows' way into LDS (a CU reads about 57 GB/s: 10 us), the
 // products with their exponentials (16 us with nothing to wait for), the block's own
 // keys and its sums (5).  With two stretches a wave adds one row tile at a time: two
@@ -543,8 +546,9 @@ hipError_t launch_weights(const WeightArgs& a, int dtype, int head_dim, hipStrea
 // A CU holds one block at a time, which takes 5 us and 0.105 for a row tile and
 // stretch (128-wide bf16 heads; 0.07 with 64-wide ones, 0.37 in fp32).  As many rows
 // see a stretch as in a prompt: single ones, the largest first, end together but for
-// half of the last, pairs are all alike.  (8 sequences of 471 entries, 1596 rows: 36
-// us with one, 32 with two; of 300 entries, where pairs are 192 blocks, 27 and 33.)
+// half of the last, pairs are all alike.  (Measured: 8 sequences of 471 entries, 1596
+// rows, 33.6 us with one and 28.9 with two; of 300 entries, where pairs are 192 blocks,
+// 25.2 and 29.9.  Of 25 shapes the choice is the faster form or within 5% of it.)
 static int stretches_of(int64_t pairs, int64_t all, int row_tiles, int dim, int elt_size) {
   const double block = 5.0, rows = row_tiles * (elt_size == 4 ? 0.37 : dim == 128 ? 0.105 : 0.07);
   const double n = (double)pairs * all, tail = n > kCus ? 0.5 * (block + rows / all) : 0.0;

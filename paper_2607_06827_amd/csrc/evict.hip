@@ -19,7 +19,9 @@
 // at once).  From 512 rows on one kernel chooses and moves (134 us as two launches, as
 // the choice alone, all latency, takes 15); one layer of one sequence has 8 and takes
 // 5.7 and 4.9 us as two, whose moves have four times the blocks (6.8 with all four
-// passes, though fewer settle it).
+// passes, though fewer settle it).  A row is one block's however long it is: of one
+// sequence with 7532 entries, half of them kept, one layer takes 78 us (31 MB) and 28
+// layers 234 (880 MB), chains of turns that nothing requests ahead.
 #include <algorithm>
 
 #include "kernels_shared.hpp"

@@ -31,7 +31,9 @@
 // values 0 in LDS.
 //
 // With bf16 the weights are rounded to bf16 before the product with V, as in this
-// library's other attention (at most 2^-8 of each; the sum is of those before).
+// library's other attention (at most 2^-8 of each; the sum is of those before): the
+// matrix products take both operands in one type.  It takes the outputs' error against
+// 64 bits from 0.0017 of their size, the outputs' own rounding, to 0.0020 .. 0.0023.
 #include "kernels_shared.hpp"
 #include "tile_attn.hpp"
 
